@@ -281,6 +281,103 @@ dynakv_status_t dynakv_export_state(dynakv_index_t* index, const dynakv_state_t*
  * zeros and appends are refused.  Counts as building the index. */
 dynakv_status_t dynakv_import_state(dynakv_index_t* index, const dynakv_state_t* src, void* stream);
 
+/* ---- Operators beside the index ------------------------------------------------------------------------------
+ * What a layer computes around its retrievals: rows of the projections are normed, rotated and laid out by unit; drafted
+ * tokens are verified against what a retrieval gathered; a packed cache holds entries in 8 or 4 bits.  The conventions
+ * above hold (device pointers of the caller, work on `stream`, no allocation, no wait).  Rows of 128 elements and the codes
+ * of a packed cache are 16-byte aligned, other arrays to their elements; outputs overlap no input. */
+
+/* Rows of one layer's projections, as dynakv_norm_rope takes them: token t of sequence b has its query heads (kv head by kv
+ * head, group_size each) at q + b * q_seq_stride + t * q_token_stride, one after the other, and its keys and values
+ * likewise; strides in elements, multiples of 8 (4 for float32). */
+typedef struct {
+  int32_t dtype;       /* dynakv_dtype_t of all rows and of the weights                              */
+  int32_t n_seqs;      /* B >= 1                                                                    */
+  int32_t n_tokens;    /* T >= 1 per sequence; n_seqs * n_tokens * heads < 2^31                      */
+  int32_t n_kv_heads;  /* H >= 1                                                                    */
+  int32_t group_size;  /* G, query heads per KV head, 1..16                                         */
+  int32_t head_dim;    /* must be 128                                                               */
+  int32_t rotary_dim;  /* leading elements of a head that are rotated: 0..128, a multiple of 8       */
+  int32_t interleaved; /* pairs of the rotation: 0: (i, i + rotary_dim / 2), 1: (2i, 2i + 1)         */
+  float eps;           /* >= 0, added to the mean square                                            */
+  int64_t q_seq_stride, q_token_stride, k_seq_stride, k_token_stride, v_seq_stride, v_token_stride;
+} dynakv_heads_t;
+
+/* Norms and rotates queries and keys and lays them out by unit, u = b * H + kv head, the layouts that dynakv_build_index,
+ * dynakv_decode_step (T = 1) and dynakv_attend_tree take; values are copied:
+ *   y = x / sqrt(mean(x^2) + eps) * weight per head, then each pair (a, b) of index i becomes
+ *   (a cos t - b sin t, b cos t + a sin t), t = position * inv_freq[i].
+ * Computed in float32 (the angle in float64), rounded once.
+ *   q, k, v             device; null: skipped, together with its output
+ *   q_weight, k_weight  device, [head_dim] in dtype, or null: no norm
+ *   inv_freq            device, float32 [rotary_dim / 2]; read only if rotary_dim > 0
+ *   positions           device, int32 [B][T]; a row with a position < 0 is padding: its outputs are left as they are
+ *   Q, K, V             device, [B * H][T][G][head_dim], [B * H][T][head_dim] twice */
+dynakv_status_t dynakv_norm_rope(const dynakv_heads_t* heads, const void* q, const void* k, const void* v,
+                                 const void* q_weight, const void* k_weight, const float* inv_freq,
+                                 const int32_t* positions, void* Q, void* K, void* V, void* stream);
+
+/* A packed cache: one row of K and one of V per unit and position, every 32 neighbouring values as integers c of `bits` bits
+ * (|c| <= 127 or 7) and one scale, a power of two: value = c * 2^(s - 127), s the scale's byte.  The writer takes the
+ * smallest scale that cuts no value off (2^e, -126 <= e; of float16: -24 <= e; so large that 127 or 7 times it still is a
+ * finite value: values beyond are held as that one) and rounds to the nearest code, ties to even.  Every value so held is exactly a value
+ * of `dtype`: what is read back is what the attention sees.  A block with a value that is not finite is held as s = 255 and is
+ * NaN throughout.  4-bit codes lie two to a byte, the even one in the low half, in two's complement, like those of 8 bits. */
+typedef struct {
+  int32_t n_units;     /* U >= 1                                                       */
+  int32_t capacity;    /* rows per unit, >= 1                                          */
+  int32_t head_dim;    /* must be 128                                                  */
+  int32_t dtype;       /* dynakv_dtype_t of what is written and read                    */
+  int32_t bits;        /* 8 or 4                                                       */
+  void* k_codes;       /* device, [U][capacity][head_dim * bits / 8]                    */
+  uint8_t* k_scales;   /* device, [U][capacity][head_dim / 32], 4-byte aligned          */
+  void* v_codes;
+  uint8_t* v_scales;
+} dynakv_packed_t;
+
+/* Quantises rows into a packed cache: row i < count[u] of unit u goes to position start[u] + i; one whose position lies
+ * outside 0..capacity-1 is dropped.
+ *   K, V   device, [U][n_tokens][head_dim] in cache->dtype; U * n_tokens < 2^31
+ *   start  device, int32 [U], or null: 0
+ *   count  device, int32 [U], or null: n_tokens (larger ones count as n_tokens) */
+dynakv_status_t dynakv_packed_write(const dynakv_packed_t* cache, const void* K, const void* V, int32_t n_tokens,
+                                    const int32_t* start, const int32_t* count, void* stream);
+
+/* Reads rows of a packed cache back: K, V device, [U][n][head_dim] in cache->dtype; row i of unit u is the one at
+ * positions[u][i].
+ *   positions  device, int32 [U][n], or null: 0..n-1; where one lies outside 0..capacity-1 the output row is left as it is */
+dynakv_status_t dynakv_packed_read(const dynakv_packed_t* cache, const int32_t* positions, int32_t n, void* K, void* V,
+                                   void* stream);
+
+/* Device scratch of the two calls below (0: invalid sizes).  One region serves any number of calls that follow each other
+ * on a stream; calls that may overlap need regions of their own. */
+size_t dynakv_tree_scratch_bytes(int32_t n_units, int32_t n_nodes, int32_t group_size);
+
+/* Attention of a tree of drafted tokens (one token: plain decoding; a chain: a chunk of a prompt) over the entries that the
+ * last retrieval of the index gathered, one softmax over those and the drafted tokens each node sees:
+ *   out[u][i][g] = softmax(scale * q . {gathered keys, K_tree[u][j] for the bits j of tree[u][i]}) . {values}
+ * The index must not have changed since that retrieval (DYNAKV_ESTATE; a captured graph holds both calls), and does not change.
+ *   Q               device, [U][n_nodes][G][head_dim] in cfg.dtype, 1 <= n_nodes <= 64
+ *   K_tree, V_tree  device, [U][n_nodes][head_dim] in cfg.dtype, or both null: the gathered entries alone
+ *   tree            device, uint64 [U][n_nodes]: bit j: node i sees drafted token j (itself included where its bit is set; bits
+ *                   from n_nodes on are ignored), or null: a chain, node i sees 0..i.  What a node does not see, NaN and
+ *                   infinities included, has no part in its output
+ *   out             device, [U][n_nodes][G][head_dim] in cfg.dtype; zeros where a node sees nothing
+ *   lse             device, float32 [U][n_nodes][G] or null: log-sum-exp of the scaled logits (-inf where it sees nothing)
+ *   scratch         device, 16-byte aligned, at least dynakv_tree_scratch_bytes(U, n_nodes, G) (else DYNAKV_ECAPACITY);
+ *                   contents need no initialisation
+ * Products and sums are float32; with 16-bit storage a probability is rounded to that type before it weights a value. */
+dynakv_status_t dynakv_attend_tree(dynakv_index_t* index, const void* Q, int32_t n_nodes, const void* K_tree,
+                                   const void* V_tree, const uint64_t* tree, void* out, float* lse, void* scratch,
+                                   size_t scratch_bytes, void* stream);
+
+/* The same over rows 0..lengths[u]-1 of a packed cache (lengths: device, int32 [U], taken into 0..capacity, or null: all);
+ * softmax_scale 0 = 1/sqrt(head_dim).  1 <= group_size <= 16. */
+dynakv_status_t dynakv_packed_attend(const dynakv_packed_t* cache, const int32_t* lengths, const void* Q, int32_t n_nodes,
+                                     int32_t group_size, const void* K_tree, const void* V_tree, const uint64_t* tree,
+                                     float softmax_scale, void* out, float* lse, void* scratch, size_t scratch_bytes,
+                                     void* stream);
+
 /* Timing aid: when enabled, the dominant kernel of dynakv_retrieve_attend / dynakv_decode_step (gather +
  * attention; where it can run, the single kernel that also scores and selects and, in a decode step,
  * appends and splits) is bracketed by HIP events on its own stream.  dynakv_profile_read synchronises those events and

@@ -48,6 +48,18 @@ class _State(C.Structure):
     _fields_ = [(k, C.c_void_p) for k in _STATE_FIELDS]
 
 
+class _Heads(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("dtype", "n_seqs", "n_tokens", "n_kv_heads", "group_size", "head_dim", "rotary_dim",
+                                          "interleaved")] + [("eps", C.c_float)] + \
+               [(k, C.c_int64) for k in ("q_seq_stride", "q_token_stride", "k_seq_stride", "k_token_stride", "v_seq_stride",
+                                          "v_token_stride")]
+
+
+class _Packed(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("n_units", "capacity", "head_dim", "dtype", "bits")] + \
+               [(k, C.c_void_p) for k in ("k_codes", "k_scales", "v_codes", "v_scales")]
+
+
 @dataclass
 class Config:
     n_units: int
@@ -96,6 +108,13 @@ def load():
         lib.dynakv_decode_step.argtypes = [vp, vp, i32, vp, vp, vp, vp, vp]
         lib.dynakv_export_state.argtypes = [vp, C.POINTER(_State), vp]
         lib.dynakv_import_state.argtypes = [vp, C.POINTER(_State), vp]
+        lib.dynakv_norm_rope.argtypes = [C.POINTER(_Heads)] + [vp] * 11
+        lib.dynakv_packed_write.argtypes = [C.POINTER(_Packed), vp, vp, i32, vp, vp, vp]
+        lib.dynakv_packed_read.argtypes = [C.POINTER(_Packed), vp, i32, vp, vp, vp]
+        lib.dynakv_tree_scratch_bytes.restype = C.c_size_t
+        lib.dynakv_tree_scratch_bytes.argtypes = [i32, i32, i32]
+        lib.dynakv_attend_tree.argtypes = [vp, vp, i32, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        lib.dynakv_packed_attend.argtypes = [C.POINTER(_Packed), vp, vp, i32, i32, vp, vp, vp, C.c_float, vp, vp, vp, C.c_size_t, vp]
         lib.dynakv_profile_enable.argtypes = [vp, i32]
         lib.dynakv_profile_sample.argtypes = [vp, i32, i32]
         lib.dynakv_profile_read.argtypes = [vp, C.POINTER(i32), C.POINTER(C.c_double)]
@@ -132,6 +151,165 @@ def _dev(t: torch.Tensor, dtype, shape=None) -> int:
     if shape is not None:
         assert tuple(t.shape) == tuple(shape), (tuple(t.shape), tuple(shape))
     return t.data_ptr()
+
+
+class _on:
+    """Makes the device of the tensors of a call current while it enqueues; value: that device's current stream."""
+
+    def __init__(self, device):
+        self.device = device
+
+    def __enter__(self):
+        self.before = torch.cuda.current_device()
+        if self.device.index != self.before:
+            torch.cuda.set_device(self.device.index)
+        return torch.cuda.current_stream(self.device.index).cuda_stream
+
+    def __exit__(self, *_):
+        if self.device.index != self.before:
+            torch.cuda.set_device(self.before)
+
+
+def _on_device(t, device, dtype, shape) -> int:
+    """Address of an operand of the operators beside the index; ValueError where it does not fit."""
+    if t.device != device or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError("expected a contiguous %s tensor %s on %s, got %s %s on %s%s" % (
+            dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device, "" if t.is_contiguous() else ", not contiguous"))
+    return t.data_ptr()
+
+
+def _gpu(t: torch.Tensor) -> torch.device:
+    if not t.is_cuda:
+        raise ValueError("expected a tensor on a GPU, got one on %s" % t.device)
+    return t.device
+
+
+# ---- operators beside the index ---------------------------------------------------------------------
+_CODES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def dynakv_norm_rope(q, k, v, positions, q_out, k_out, v_out, q_weight=None, k_weight=None, inv_freq=None, eps=1e-6,
+                     interleaved=False):
+    """Norms, rotates and lays out a layer's projected rows by unit (see the header).
+
+    q [B, T, H * G, 128], k and v [B, T, H, 128]: views whose last two dimensions are contiguous (parts of one fused projection
+    are); any of them may be None together with its output.  positions int32 [B, T], negative: padding, left as it is.
+    q_out [B * H, T, G, 128], k_out and v_out [B * H, T, 128]; q_weight, k_weight [128] or None: no norm; inv_freq float32
+    [rotary_dim / 2] or None: no rotation."""
+    given = [(x, o) for x, o in ((q, q_out), (k, k_out), (v, v_out)) if x is not None]
+    if not given or any((x is None) != (o is None) for x, o in ((q, q_out), (k, k_out), (v, v_out))):
+        raise ValueError("queries, keys and values each come with their output")
+    first = given[0][0]
+    device, dtype = _gpu(first), first.dtype
+    if dtype not in _CODES:
+        raise ValueError("rows of %s are not supported" % dtype)
+    B, T = positions.shape
+    kv = k if k is not None else v
+    H = kv.shape[2] if kv is not None else q_out.shape[0] // max(1, B)
+    if H < 1 or (q is not None and (q.shape[2] % H or q.shape[2] == 0)):
+        raise ValueError("%d query heads do not go with %d KV heads" % (q.shape[2], H))
+    G = q.shape[2] // H if q is not None else 1
+    c = _Heads(_CODES[dtype], B, T, H, G, 128, 0 if inv_freq is None else 2 * inv_freq.numel(), int(bool(interleaved)), eps)
+    for name, x, heads in (("q", q, H * G), ("k", k, H), ("v", v, H)):
+        if x is None:
+            continue
+        # a dimension of one element may have any stride
+        if x.device != device or x.dtype != dtype or x.shape != (B, T, heads, 128) or x.stride(3) != 1 or (heads > 1 and x.stride(2) != 128):
+            raise ValueError("%s: expected %s [%d, %d, %d, 128] on %s with contiguous heads, got %s %s, strides %s, on %s" % (
+                name, dtype, B, T, heads, device, x.dtype, tuple(x.shape), x.stride(), x.device))
+        setattr(c, name + "_seq_stride", x.stride(0) if B > 1 else 0)
+        setattr(c, name + "_token_stride", x.stride(1) if T > 1 else 0)
+    ptr = lambda x: None if x is None else x.data_ptr()  # noqa: E731
+    opt = lambda x, dt, shape: None if x is None else _on_device(x, device, dt, shape)  # noqa: E731
+    if inv_freq is not None and inv_freq.dim() != 1:
+        raise ValueError("inv_freq has one dimension, got %s" % (tuple(inv_freq.shape),))
+    out = (opt(q_out, dtype, (B * H, T, G, 128)), opt(k_out, dtype, (B * H, T, 128)), opt(v_out, dtype, (B * H, T, 128)))
+    wq, wk = opt(q_weight, dtype, (128,)), opt(k_weight, dtype, (128,))
+    freq, pos = opt(inv_freq, torch.float32, inv_freq.shape if inv_freq is not None else None), _on_device(positions, device, torch.int32, (B, T))
+    lib = load()
+    with _on(device) as stream:
+        _check(lib.dynakv_norm_rope(C.byref(c), ptr(q), ptr(k), ptr(v), wq, wk, freq, pos, *out, stream), "dynakv_norm_rope")
+
+
+def dynakv_tree_scratch_bytes(n_units: int, n_nodes: int, group_size: int) -> int:
+    return load().dynakv_tree_scratch_bytes(n_units, n_nodes, group_size)
+
+
+def tree_scratch(n_units: int, n_nodes: int, group_size: int, device="cuda:0") -> torch.Tensor:
+    """Scratch for dynakv_attend_tree and dynakv_packed_attend of these sizes.  Calls that may overlap (two streams, two graphs)
+    need one each."""
+    n = dynakv_tree_scratch_bytes(n_units, n_nodes, group_size)
+    if n == 0:
+        raise ValueError("dynakv: no tree of %d nodes with %d query heads on %d units" % (n_nodes, group_size, n_units))
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _tree_operands(device, dtype, U, Q, k_tree, v_tree, tree, out, lse, scratch):
+    """Addresses of what the two attentions of drafted tokens share, in the order of their arguments around the scale."""
+    if Q.dim() != 4 or (k_tree is None) != (v_tree is None):
+        raise ValueError("Q is [units, nodes, query heads, 128]; drafted keys and values come together")
+    T, G = Q.shape[1], Q.shape[2]
+    opt = lambda x, dt, shape: None if x is None else _on_device(x, device, dt, shape)  # noqa: E731
+    q, o = _on_device(Q, device, dtype, (U, T, G, 128)), _on_device(out, device, dtype, (U, T, G, 128))
+    if scratch.device != device or scratch.dtype != torch.uint8 or not scratch.is_contiguous():
+        raise ValueError("scratch: expected contiguous bytes on %s" % device)
+    return (T, G, q, opt(k_tree, dtype, (U, T, 128)), opt(v_tree, dtype, (U, T, 128)), opt(tree, torch.int64, (U, T)), o,
+            opt(lse, torch.float32, (U, T, G)), scratch.data_ptr(), scratch.numel())
+
+
+class PackedCache:
+    """A packed cache (dynakv_packed_t) over four uint8 tensors that it keeps alive: codes [U, capacity, 128 * bits / 8] and
+    scales [U, capacity, 4] of keys and of values; dtype "f32", "f16" or "bf16": of what is written and read."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales, dtype: str):
+        self._lib = load()
+        self.device = _gpu(k_codes)
+        if k_codes.dim() != 3 or k_codes.shape[2] not in (128, 64) or dtype not in DTYPES:
+            raise ValueError("codes are [units, capacity, 128 or 64] of dtype f32, f16 or bf16, got %s, %s" % (tuple(k_codes.shape), dtype))
+        U, cap, width = k_codes.shape
+        self.n_units, self.capacity, self.bits, self.dtype = U, cap, width // 16, TORCH_DTYPES[dtype]
+        u8 = torch.uint8
+        self.tensors = (k_codes, k_scales, v_codes, v_scales)
+        self._c = _Packed(U, cap, 128, DTYPES[dtype], self.bits, _on_device(k_codes, self.device, u8, (U, cap, width)),
+                          _on_device(k_scales, self.device, u8, (U, cap, 4)), _on_device(v_codes, self.device, u8, (U, cap, width)),
+                          _on_device(v_scales, self.device, u8, (U, cap, 4)))
+        self._ref = C.byref(self._c)
+
+    @classmethod
+    def zeros(cls, n_units: int, capacity: int, dtype: str, bits: int, device="cuda:0"):
+        if bits not in (8, 4):
+            raise ValueError("a packed cache has 8 or 4 bits, not %r" % (bits,))
+        t = [torch.zeros(n_units, capacity, w, dtype=torch.uint8, device=device) for w in (16 * bits, 4, 16 * bits, 4)]
+        return cls(*t, dtype=dtype)
+
+    def _rows(self, K, V):
+        if K.dim() != 3:
+            raise ValueError("rows are [units, tokens, 128], got %s" % (tuple(K.shape),))
+        n = K.shape[1]
+        return n, _on_device(K, self.device, self.dtype, (self.n_units, n, 128)), _on_device(V, self.device, self.dtype, (self.n_units, n, 128))
+
+    def dynakv_packed_write(self, K: torch.Tensor, V: torch.Tensor, start: torch.Tensor | None = None, count: torch.Tensor | None = None):
+        """Row i < count[u] of K, V [U, n, 128] goes to position start[u] + i (int32 [U]; None: 0 and n)."""
+        n, kp, vp = self._rows(K, V)
+        sp = None if start is None else _on_device(start, self.device, torch.int32, (self.n_units,))
+        cp = None if count is None else _on_device(count, self.device, torch.int32, (self.n_units,))
+        with _on(self.device) as stream:
+            _check(self._lib.dynakv_packed_write(self._ref, kp, vp, n, sp, cp, stream), "dynakv_packed_write")
+
+    def dynakv_packed_read(self, positions: torch.Tensor | None, K: torch.Tensor, V: torch.Tensor):
+        """The rows at positions (int32 [U, n]; None: the first n) into K, V [U, n, 128]."""
+        n, kp, vp = self._rows(K, V)
+        pp = None if positions is None else _on_device(positions, self.device, torch.int32, (self.n_units, n))
+        with _on(self.device) as stream:
+            _check(self._lib.dynakv_packed_read(self._ref, pp, n, kp, vp, stream), "dynakv_packed_read")
+
+    def dynakv_packed_attend(self, lengths, Q, k_tree, v_tree, tree, out, lse, scratch, softmax_scale: float = 0.0):
+        """Attention of a tree of drafted tokens over rows 0..lengths[u]-1 (int32 [U]; None: all); operands as those of
+        Index.dynakv_attend_tree."""
+        lp = None if lengths is None else _on_device(lengths, self.device, torch.int32, (self.n_units,))
+        T, G, q, k, v, t, o, l, s, n = _tree_operands(self.device, self.dtype, self.n_units, Q, k_tree, v_tree, tree, out, lse, scratch)
+        with _on(self.device) as stream:
+            _check(self._lib.dynakv_packed_attend(self._ref, lp, q, T, G, k, v, t, softmax_scale, o, l, s, n, stream), "dynakv_packed_attend")
 
 
 class Index:
@@ -225,6 +403,17 @@ class Index:
         vp = _dev(v_new, self._tdtype, (c.n_units, c.head_dim))
         _check(self._lib.dynakv_decode_step(self._h, qp, int(token_budget), op, lp, kp, vp, _stream()),
                "dynakv_decode_step")
+
+    def dynakv_attend_tree(self, Q, k_tree, v_tree, tree, out, lse, scratch):
+        """Attention of a tree of drafted tokens over what the last retrieval gathered, and over the tree.
+
+        Q, out [U, nodes, G, 128]; k_tree, v_tree [U, nodes, 128] or None; tree int64 [U, nodes] of which bit j says that the
+        node sees drafted token j, or None: a chain; lse float32 [U, nodes, G] or None; scratch: tree_scratch(U, nodes, G)."""
+        T, G, q, k, v, t, o, l, s, n = _tree_operands(self.workspace.device, self._tdtype, self.cfg.n_units, Q, k_tree, v_tree, tree, out, lse, scratch)
+        if G != self.cfg.group_size:
+            raise ValueError("the index has %d query heads per unit, Q %d" % (self.cfg.group_size, G))
+        with _on(self.workspace.device) as stream:
+            _check(self._lib.dynakv_attend_tree(self._h, q, T, k, v, t, o, l, s, n, stream), "dynakv_attend_tree")
 
     def decode_step_ptrs(self, q_ptr: int, budget: int, out_ptr: int, lse_ptr: int, k_ptr: int, v_ptr: int, stream: int):
         """dynakv_decode_step on raw device addresses, without per-call tensor checks, for loops where

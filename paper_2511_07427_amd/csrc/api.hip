@@ -7,6 +7,7 @@
 #include <vector>
 
 #include "common.hpp"
+#include "operators.hpp"
 
 using namespace dynakv;
 
@@ -17,6 +18,8 @@ struct dynakv_index {
   size_t bytes;
   bool built;
   int local_count;   // local update: appends enqueued since the last local clustering
+  bool listed;       // the gather list is that of a retrieval since which the index has not changed
+  int list_budget;   // its token budget
   // optional timing of the gather + attention kernel
   bool profiling;
   std::vector<hipEvent_t> ev;   // start/stop pairs
@@ -182,6 +185,8 @@ dynakv_status_t dynakv_create(const dynakv_config_t* cfg, void* workspace, size_
   ix->bytes = carve(*cfg, (char*)workspace, &ix->view);
   ix->built = false;
   ix->local_count = 0;
+  ix->listed = false;
+  ix->list_budget = 0;
   ix->profiling = false;
   ix->n_prof = 0;
   *out = ix;
@@ -199,6 +204,7 @@ dynakv_status_t dynakv_build_index(dynakv_index_t* ix, const void* K, const void
                                    const int32_t* init_idx, void* stream) {
   if (!ix || !K || !V || !init_idx) return DYNAKV_EINVAL;
   if (n_tokens < ix->cfg.n_clusters_init || n_tokens > ix->cfg.max_tokens || n_tokens > kMaxPrefill) return DYNAKV_EINVAL;
+  ix->listed = false;
   const hipError_t e = launch_build_index(ix->view, K, V, n_tokens, init_idx, ix->cfg.kmeans_iters, ix->workspace,
                                           ix->bytes, (hipStream_t)stream);
   if (e != hipSuccess) return DYNAKV_EHIP;
@@ -215,6 +221,7 @@ static dynakv_status_t retrieve_impl(dynakv_index_t* ix, const View& view, const
                                      bool* appended) {
   const bool fused = retrieve_is_fused(view);
   *appended = fused && kin;
+  ix->listed = false;                                // (until the retrieval is enqueued)
   if (!fused && launch_score_select(view, Q, token_budget, kin, st) != hipSuccess) return DYNAKV_EHIP;
   const int phase = ix->profiling ? (int)(ix->prof_seen++ % ix->prof_every) : -1;
   const bool prof = phase >= 0 && phase < ix->prof_run && 2 * (ix->n_prof + 1) <= (int)ix->ev.size();
@@ -230,6 +237,8 @@ static dynakv_status_t retrieve_impl(dynakv_index_t* ix, const View& view, const
       ++ix->n_prof;
     }
   }
+  ix->listed = !*appended;
+  ix->list_budget = token_budget;
   return DYNAKV_OK;
 }
 
@@ -295,10 +304,12 @@ dynakv_status_t dynakv_decode_step(dynakv_index_t* ix, const void* Q, int32_t to
   if (ix->view.token_level) {                        // no nearest-cluster search, no splits
     const dynakv_status_t rc = retrieve_impl(ix, ix->view, Q, token_budget, out, lse, nullptr, nullptr, false, st, &appended);
     if (rc != DYNAKV_OK) return rc;
+    ix->listed = false;
     return append_own_cluster(ix, k_new, v_new, st);
   }
   const bool one_kernel = ix->view.fuse == 2;        // the splits too, where the retrieval kernel takes the append
   const dynakv_status_t rc = retrieve_impl(ix, ix->view, Q, token_budget, out, lse, k_new, v_new, one_kernel, st, &appended);
+  ix->listed = false;
   if (rc != DYNAKV_OK) return rc;
   if (appended && one_kernel) return DYNAKV_OK;
   // separate kernels: the score kernel of this step has already looked for the new key's nearest cluster, and the
@@ -310,6 +321,7 @@ dynakv_status_t dynakv_decode_step(dynakv_index_t* ix, const void* Q, int32_t to
 dynakv_status_t dynakv_append(dynakv_index_t* ix, const void* k_new, const void* v_new, void* stream) {
   if (!ix || !k_new || !v_new) return DYNAKV_EINVAL;
   if (!ix->built) return DYNAKV_ESTATE;
+  ix->listed = false;
   if (ix->view.token_level) return append_own_cluster(ix, k_new, v_new, (hipStream_t)stream);
   return launch_append(ix->view, k_new, v_new, false, false, (hipStream_t)stream) == hipSuccess ? DYNAKV_OK : DYNAKV_EHIP;
 }
@@ -318,6 +330,7 @@ dynakv_status_t dynakv_extend_index(dynakv_index_t* ix, const void* K, const voi
   if (!ix || !K || !V || n_tokens < 1) return DYNAKV_EINVAL;
   if (!ix->built) return DYNAKV_ESTATE;
   if (ix->view.token_level) return DYNAKV_EINVAL;
+  ix->listed = false;
   View v = ix->view;
   v.Bmax = 0;                                        // the chunk is resident: flagged clusters are split at once
   return launch_extend(v, K, V, n_tokens, (hipStream_t)stream) == hipSuccess ? DYNAKV_OK : DYNAKV_EHIP;
@@ -329,6 +342,7 @@ dynakv_status_t dynakv_place_by_coretrieval(dynakv_index_t* ix, const void* K, c
   if (!ix || !K || !V || !Qref || !P || n_ref < 1 || token_budget < 0) return DYNAKV_EINVAL;
   if (n_tokens < ix->cfg.n_clusters_init || n_tokens > ix->cfg.max_tokens) return DYNAKV_EINVAL;
   if (!ix->built) return DYNAKV_ESTATE;
+  ix->listed = false;
   return launch_place(ix->view, K, V, n_tokens, Qref, n_ref, token_budget, P, order, (hipStream_t)stream) == hipSuccess
              ? DYNAKV_OK : DYNAKV_EHIP;
 }
@@ -337,6 +351,7 @@ dynakv_status_t dynakv_split(dynakv_index_t* ix, void* stream) {
   if (!ix) return DYNAKV_EINVAL;
   if (!ix->built) return DYNAKV_ESTATE;
   if (ix->view.token_level || ix->view.static_update) return DYNAKV_OK;       // nothing is ever flagged
+  ix->listed = false;
   return launch_split(ix->view, (hipStream_t)stream) == hipSuccess ? DYNAKV_OK : DYNAKV_EHIP;
 }
 
@@ -360,10 +375,108 @@ dynakv_status_t dynakv_import_state(dynakv_index_t* ix, const dynakv_state_t* sr
       !src->m2 || !src->offsets || !src->members || !src->keys || !src->values)
     return DYNAKV_EINVAL;
   if ((src->n_selected == nullptr) != (src->selected == nullptr)) return DYNAKV_EINVAL;
+  ix->listed = false;
   if (launch_import(ix->view, *src, !ix->built, (hipStream_t)stream) != hipSuccess) return DYNAKV_EHIP;
   ix->built = true;
   ix->local_count = 0;
   return DYNAKV_OK;
+}
+
+// ---- operators beside the index ----------------------------------------------------------------------
+static bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+static bool dtype_ok(int dtype) { return dtype == DYNAKV_F32 || dtype == DYNAKV_F16 || dtype == DYNAKV_BF16; }
+
+dynakv_status_t dynakv_norm_rope(const dynakv_heads_t* heads, const void* q, const void* k, const void* v, const void* q_weight,
+                                 const void* k_weight, const float* inv_freq, const int32_t* positions, void* Q, void* K, void* V,
+                                 void* stream) {
+  if (!heads || !positions || !aligned(positions, 4)) return DYNAKV_EINVAL;
+  const dynakv_heads_t& c = *heads;
+  if (!dtype_ok(c.dtype) || c.head_dim != kHeadDim || c.n_seqs < 1 || c.n_tokens < 1 || c.n_kv_heads < 1) return DYNAKV_EINVAL;
+  if (c.group_size < 1 || c.group_size > 16 || c.interleaved < 0 || c.interleaved > 1) return DYNAKV_EINVAL;
+  if (c.rotary_dim < 0 || c.rotary_dim > kHeadDim || c.rotary_dim % 8 || (c.rotary_dim && (!inv_freq || !aligned(inv_freq, 4)))) return DYNAKV_EINVAL;
+  if (!(c.eps >= 0.f && c.eps <= 3.4e38f)) return DYNAKV_EINVAL;
+  if ((!q) != (!Q) || (!k) != (!K) || (!v) != (!V)) return DYNAKV_EINVAL;
+  const unsigned __int128 rows = (unsigned __int128)((unsigned long long)c.n_seqs * c.n_tokens) * ((unsigned long long)c.n_kv_heads * (c.group_size + 2));
+  if (rows >= ((unsigned __int128)1 << 31) || (long long)c.n_kv_heads * (c.group_size + 2) > (1 << 19)) return DYNAKV_EINVAL;
+  const int64_t step = 16 / elem_size(c.dtype);
+  const void* rows_of[] = {q, k, v, q_weight, k_weight, Q, K, V};
+  for (const void* p : rows_of)
+    if (!aligned(p, 16)) return DYNAKV_EINVAL;
+  const struct { const void* p; int64_t seq, token; } in[] = {
+      {q, c.q_seq_stride, c.q_token_stride}, {k, c.k_seq_stride, c.k_token_stride}, {v, c.v_seq_stride, c.v_token_stride}};
+  for (const auto& s : in)
+    if (s.p && (s.seq % step || s.token % step)) return DYNAKV_EINVAL;
+  if (!q && !k && !v) return DYNAKV_OK;
+  HeadsArgs a = {c, q, k, v, q_weight, k_weight, inv_freq, positions, Q, K, V, 1};
+  return launch_norm_rope(a, (hipStream_t)stream) == hipSuccess ? DYNAKV_OK : DYNAKV_EHIP;
+}
+
+static bool packed_ok(const dynakv_packed_t* c) {
+  return c && c->n_units >= 1 && c->capacity >= 1 && c->head_dim == kHeadDim && dtype_ok(c->dtype) && (c->bits == 8 || c->bits == 4) &&
+         c->k_codes && c->v_codes && c->k_scales && c->v_scales && aligned(c->k_codes, 16) && aligned(c->v_codes, 16) &&
+         aligned(c->k_scales, 4) && aligned(c->v_scales, 4);
+}
+
+dynakv_status_t dynakv_packed_write(const dynakv_packed_t* cache, const void* K, const void* V, int32_t n_tokens, const int32_t* start,
+                                    const int32_t* count, void* stream) {
+  if (!packed_ok(cache) || !K || !V || n_tokens < 0 || !aligned(K, 16) || !aligned(V, 16) || !aligned(start, 4) || !aligned(count, 4)) return DYNAKV_EINVAL;
+  if ((long long)cache->n_units * n_tokens >= (1ll << 31)) return DYNAKV_EINVAL;
+  if (n_tokens == 0) return DYNAKV_OK;
+  return launch_packed_write(*cache, K, V, n_tokens, start, count, (hipStream_t)stream) == hipSuccess ? DYNAKV_OK : DYNAKV_EHIP;
+}
+
+dynakv_status_t dynakv_packed_read(const dynakv_packed_t* cache, const int32_t* positions, int32_t n, void* K, void* V, void* stream) {
+  if (!packed_ok(cache) || !K || !V || n < 0 || !aligned(K, 16) || !aligned(V, 16) || !aligned(positions, 4)) return DYNAKV_EINVAL;
+  if ((long long)cache->n_units * n >= (1ll << 31)) return DYNAKV_EINVAL;
+  if (n == 0) return DYNAKV_OK;
+  return launch_packed_read(*cache, positions, n, K, V, (hipStream_t)stream) == hipSuccess ? DYNAKV_OK : DYNAKV_EHIP;
+}
+
+size_t dynakv_tree_scratch_bytes(int32_t n_units, int32_t n_nodes, int32_t group_size) {
+  if (n_units < 1 || n_nodes < 1 || n_nodes > kMaxNodes || group_size < 1 || group_size > 16) return 0;
+  return tree_scratch_bytes(n_units, n_nodes, group_size);
+}
+
+// What both attentions take besides the entries.
+static dynakv_status_t tree_args(TreeArgs* a, int U, int T, int G, int dtype, float scale, const void* Q, const void* K1, const void* V1,
+                                 const uint64_t* tree, void* out, float* lse, void* scratch, size_t scratch_bytes) {
+  if (!Q || !out || !scratch || (!K1) != (!V1) || T < 1 || T > kMaxNodes || G < 1 || G > 16) return DYNAKV_EINVAL;
+  if (!aligned(Q, 16) || !aligned(K1, 16) || !aligned(V1, 16) || !aligned(out, 16) || !aligned(scratch, 16) || !aligned(tree, 8) || !aligned(lse, 4))
+    return DYNAKV_EINVAL;
+  if ((long long)U * T * G >= (1ll << 31)) return DYNAKV_EINVAL;
+  if (scratch_bytes < tree_scratch_bytes(U, T, G)) return DYNAKV_ECAPACITY;
+  a->U = U; a->T = T; a->G = G; a->dtype = dtype;
+  a->sc = scale * 1.4426950408889634f;
+  a->Q = Q; a->K1 = K1; a->V1 = V1; a->tree = (const unsigned long long*)tree;
+  a->out = out; a->lse = lse; a->part = (float*)scratch;
+  return DYNAKV_OK;
+}
+
+dynakv_status_t dynakv_attend_tree(dynakv_index_t* ix, const void* Q, int32_t n_nodes, const void* K_tree, const void* V_tree,
+                                   const uint64_t* tree, void* out, float* lse, void* scratch, size_t scratch_bytes, void* stream) {
+  if (!ix) return DYNAKV_EINVAL;
+  const View& v = ix->view;
+  TreeArgs a = {};
+  const dynakv_status_t rc = tree_args(&a, v.U, n_nodes, v.G, v.dtype, v.scale_f, Q, K_tree, V_tree, tree, out, lse, scratch, scratch_bytes);
+  if (rc != DYNAKV_OK) return rc;
+  if (!ix->built || !ix->listed) return DYNAKV_ESTATE;
+  a.pages = v.pages; a.unit_pages = (size_t)v.Pcap * kPageElems * elem_size(v.dtype);
+  a.plist = v.plist; a.n_list = v.n_list; a.Lcap = v.Lcap;
+  a.most = std::min(ix->list_budget, v.Ncap);
+  return launch_tree(a, (hipStream_t)stream) == hipSuccess ? DYNAKV_OK : DYNAKV_EHIP;
+}
+
+dynakv_status_t dynakv_packed_attend(const dynakv_packed_t* cache, const int32_t* lengths, const void* Q, int32_t n_nodes, int32_t group_size,
+                                     const void* K_tree, const void* V_tree, const uint64_t* tree, float softmax_scale, void* out, float* lse,
+                                     void* scratch, size_t scratch_bytes, void* stream) {
+  if (!packed_ok(cache) || !aligned(lengths, 4) || !(softmax_scale >= 0.f && softmax_scale <= 3.4e38f)) return DYNAKV_EINVAL;
+  TreeArgs a = {};
+  const float scale = softmax_scale > 0.f ? softmax_scale : (float)(1.0 / std::sqrt((double)kHeadDim));
+  const dynakv_status_t rc = tree_args(&a, cache->n_units, n_nodes, group_size, cache->dtype, scale, Q, K_tree, V_tree, tree, out, lse, scratch,
+                                       scratch_bytes);
+  if (rc != DYNAKV_OK) return rc;
+  a.cache = *cache; a.lengths = lengths; a.most = cache->capacity;
+  return launch_tree(a, (hipStream_t)stream) == hipSuccess ? DYNAKV_OK : DYNAKV_EHIP;
 }
 
 dynakv_status_t dynakv_profile_enable(dynakv_index_t* ix, int32_t max_launches) {

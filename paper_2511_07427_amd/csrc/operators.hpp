@@ -1,0 +1,58 @@
+// Arguments and launchers of the operators beside the index: heads.hip, packed.hip, tree.hip.
+#pragma once
+
+#include "common.hpp"
+
+namespace dynakv {
+
+struct HeadsArgs {
+  dynakv_heads_t c;
+  const void *q, *k, *v, *wq, *wk;
+  const float* inv_freq;
+  const int* positions;
+  void *Q, *K, *V;
+  int per;   // rows of a token that each row of 16 lanes works on
+};
+hipError_t launch_norm_rope(const HeadsArgs& a, hipStream_t st);
+
+// ---- packed cache ---------------------------------------------------------------------------------------------
+constexpr int kBlock = 32;                          // values that share a scale
+constexpr int kRowScales = kHeadDim / kBlock;       // scale bytes of a row
+__host__ __device__ inline int code_bytes(int bits) { return kHeadDim * bits / 8; }
+// Scale byte -> 2^(s - 127); 255: NaN.
+__device__ __forceinline__ float scale_value(uint32_t s) {
+  return __uint_as_float(s == 255u ? 0x7FC00000u : s ? s << 23 : 0x00400000u);
+}
+hipError_t launch_packed_write(const dynakv_packed_t& c, const void* K, const void* V, int n, const int* start, const int* count,
+                               hipStream_t st);
+hipError_t launch_packed_read(const dynakv_packed_t& c, const int* positions, int n, void* K, void* V, hipStream_t st);
+
+// ---- attention of drafted tokens --------------------------------------------------------------------------------
+constexpr int kMaxNodes = 64;                       // one bit each in a node's word of the tree
+struct TreeArgs {
+  int U, T, G, dtype;
+  float sc;                                         // softmax scale * log2(e)
+  const void *Q, *K1, *V1;
+  const unsigned long long* tree;                   // null: a chain
+  void* out;
+  float* lse;
+  float* part;                                      // [U][S][T * G][kPartRow]
+  int most;                                         // no unit has more entries than this, as far as the host knows
+  // the entries: the gather list of an index ...
+  const char* pages;                                // null: a packed cache
+  size_t unit_pages;                                // bytes of a unit's page pool
+  const int *plist, *n_list;
+  int Lcap;
+  // ... or rows of a packed cache
+  dynakv_packed_t cache;
+  const int* lengths;
+  // launch shape (plan_tree)
+  int S;                                            // most workgroups that share the entries of a unit
+  int RB;                                           // blocks of rows
+  int chunk;                                        // entries that a workgroup takes at least, where several share a unit
+};
+constexpr int kPartRow = kHeadDim + 4;              // accumulators, maximum, denominator, padding to 16 bytes
+size_t tree_scratch_bytes(int U, int T, int G);
+hipError_t launch_tree(const TreeArgs& a, hipStream_t st);
+
+}  // namespace dynakv
