@@ -8,8 +8,10 @@
 // the probabilities are, as they lie in the registers, the B operand of O^T += V^T P^T: the matrix instruction sums over
 // entries in whatever order both operands agree on.  V comes out of LDS transposed by the LDS's transposing read.
 //
-// K and V tiles lie in LDS row by row, 16-byte chunk c of row r at position c ^ fz(r): 16 rows at one chunk (K) and 4 rows
-// at 4 neighbouring chunks (V) each fall on different banks.
+// K and V tiles lie in LDS row by row, padded so that the lanes served together fall on different banks: 16 rows at one 16-byte
+// chunk of K (pad 16: rows 4 banks apart), 4 rows at 32 neighbouring bytes of V (pad 32: rows 8 banks apart).  Padding, unlike a
+// permutation of the chunks, leaves every place of a tile at a constant distance from one address per lane: a permutation cost some
+// 40 registers of addresses, which the accumulators need.
 #include "operators.hpp"
 
 namespace dynakv {
@@ -20,18 +22,23 @@ typedef float f16v __attribute__((ext_vector_type(16)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef short s4 __attribute__((ext_vector_type(4)));
+typedef float f2v __attribute__((ext_vector_type(2)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kSub = 32;                             // entries of one matrix tile, rows of a wavefront
 
-__device__ __forceinline__ int fz(int row) { return ((row & 3) << 2) | ((row >> 2) & 3); }
+// Keeps the loads of what follows from being moved up in front of what came before, where their results fill the registers.
+__device__ __forceinline__ void hold_order() { __builtin_amdgcn_sched_barrier(0); }
+
 // entry of accumulator register i of the lanes of half h
 __device__ __forceinline__ constexpr int entry_of(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
 
 // Matrix products of one storage type.  Rows of a tile are kRow bytes.
 template <int DT>
 struct Mma {
-  static constexpr int kES = 2, kRow = kHeadDim * 2;
+  static constexpr int kES = 2, kRow = kHeadDim * 2, kRowK = kRow + 16, kRowV = kRow + 32;   // in memory, in LDS
   struct Q { uint4 b[8]; };
   static __device__ __forceinline__ void load_q(Q& q, const void* base, size_t row, int h, bool ok) {
     const char* p = (const char*)base + row * kRow + 16 * h;
@@ -44,47 +51,57 @@ struct Mma {
     else
       return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
   }
-  static __device__ __forceinline__ f16v qk(const char* k, const Q& q, int lane) {
-    const int t = lane & 31, x = ((lane >> 5) ^ fz(t)) << 4;
-    f16v c = {};
+  // scores of N tiles of 32 entries each, kSub rows apart
+  template <int N>
+  static __device__ __forceinline__ void qk(f16v (&c)[N], const char* k, const Q& q, int lane) {
+    const char* at = k + (lane & 31) * kRowK + (lane >> 5) * 16;
 #pragma unroll
-    for (int s = 0; s < 8; ++s) c = mma(*(const uint4*)(k + t * kRow + (x ^ (s << 5))), q.b[s], c);
-    return c;
+    for (int n = 0; n < N; ++n) c[n] = f16v{};
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) c[n] = mma(*(const uint4*)(at + n * kSub * kRowK + s * 32), q.b[s], c[n]);
+      if (s % 4 == 3) hold_order();
+    }
   }
   static __device__ __forceinline__ uint16_t round16(float x) {
     if constexpr (DT == DYNAKV_BF16) return __builtin_bit_cast(uint16_t, (__bf16)x);
     else return __builtin_bit_cast(uint16_t, (_Float16)x);
   }
+  static __device__ __forceinline__ uint32_t round2(float x, float y) {
+    if constexpr (DT == DYNAKV_BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2v){x, y}, b2));
+    else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2v){x, y}, h2));
+  }
   static __device__ __forceinline__ void pv(f16v (&o)[4], const char* v, const float (&p)[16], int lane) {
-    const int h = lane >> 5, g = (lane >> 4) & 1, j = lane & 15;
+    // a group of 16 lanes reads 4 entries (rows) of 16 columns and gets the 4 entries of one column per lane
+    const int j = lane & 15;
+    const char* from = v + ((lane >> 5) * 4 + (j >> 2)) * kRowV + ((lane >> 4) & 1) * 32 + (j & 3) * 8;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       // the probability that weights V goes in rounded to V's type: an error of half a step relative to each term, as much
       // as rounding the output costs
       uint32_t w[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) w[k] = round16(p[8 * c + 2 * k]) | ((uint32_t)round16(p[8 * c + 2 * k + 1]) << 16);
+      for (int k = 0; k < 4; ++k) w[k] = round2(p[8 * c + 2 * k], p[8 * c + 2 * k + 1]);
       const uint4 b = {w[0], w[1], w[2], w[3]};
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         uint2 a[2];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          // a group of 16 lanes reads 4 entries (rows) of 16 columns and gets the 4 entries of one column per lane
-          const int row = 16 * c + 8 * x + 4 * h + (j >> 2), chunk = 4 * d + 2 * g + ((j & 3) >> 1);
-          const char* at = v + row * kRow + ((chunk ^ (((j >> 2) << 2) | (2 * x + h))) << 4) + (j & 1) * 8;
-          a[x] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)at));
-        }
+        for (int x = 0; x < 2; ++x)
+          a[x] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                               (__attribute__((address_space(3))) s4*)(from + (16 * c + 8 * x) * kRowV + d * 64)));
         o[d] = mma(uint4{a[0].x, a[0].y, a[1].x, a[1].y}, b, o[d]);
       }
+      hold_order();
     }
   }
   static __device__ __forceinline__ float elem(const void* base, size_t i) { return load_elem(base, i, DT); }
   // four consecutive columns of an output row
   static __device__ __forceinline__ void store4(void* out, size_t i, f4 x) {
-    *(uint2*)((uint16_t*)out + i) = uint2{round16(x[0]) | ((uint32_t)round16(x[1]) << 16), round16(x[2]) | ((uint32_t)round16(x[3]) << 16)};
+    *(uint2*)((uint16_t*)out + i) = uint2{round2(x[0], x[1]), round2(x[2], x[3])};
   }
-  // whether one of the elements of a chunk is no finite number
+  // a chunk with zeros for the elements that are no finite numbers; bad: there was one
   static __device__ __forceinline__ uint4 only_finite(uint4 a, bool& bad) {
     constexpr uint32_t ex = DT == DYNAKV_BF16 ? 0x7F80u : 0x7C00u;
     uint32_t* w = (uint32_t*)&a;
@@ -99,34 +116,38 @@ struct Mma {
 
 template <>
 struct Mma<DYNAKV_F32> {
-  static constexpr int kES = 4, kRow = kHeadDim * 4;
+  static constexpr int kES = 4, kRow = kHeadDim * 4, kRowK = kRow + 16, kRowV = kRow + 32;
   struct Q { f4 b[16]; };
   static __device__ __forceinline__ void load_q(Q& q, const void* base, size_t row, int h, bool ok) {
     const char* p = (const char*)base + row * kRow + 16 * h;
 #pragma unroll
     for (int s = 0; s < 16; ++s) q.b[s] = ok ? *(const f4*)(p + 32 * s) : f4{0, 0, 0, 0};
   }
-  static __device__ __forceinline__ f16v qk(const char* k, const Q& q, int lane) {
-    const int t = lane & 31, x = ((lane >> 5) ^ fz(t)) << 4;
-    f16v c = {};
+  template <int N>
+  static __device__ __forceinline__ void qk(f16v (&c)[N], const char* k, const Q& q, int lane) {
+    const char* at = k + (lane & 31) * kRowK + (lane >> 5) * 16;
 #pragma unroll
-    for (int s = 0; s < 16; ++s) {
-      const f4 a = *(const f4*)(k + t * kRow + (x ^ (s << 5)));
+    for (int n = 0; n < N; ++n) c[n] = f16v{};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], q.b[s][i], c, 0, 0, 0);
-    }
-    return c;
+    for (int s = 0; s < 16; ++s)
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const f4 a = *(const f4*)(at + n * kSub * kRowK + s * 32);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], q.b[s][i], c[n], 0, 0, 0);
+        if (s % 4 == 3) hold_order();
+      }
   }
   static __device__ __forceinline__ void pv(f16v (&o)[4], const char* v, const float (&p)[16], int lane) {
-    const int h = lane >> 5, col = lane & 31;
+    const char* from = v + (lane >> 5) * 4 * kRowV + (lane & 31) * 4;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const int row = entry_of(i, h);
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
-        const float a = *(const float*)(v + row * kRow + (((8 * d + (col >> 2)) ^ fz(row)) << 4) + ((col & 3) << 2));
+        const float a = *(const float*)(from + entry_of(i, 0) * kRowV + d * 128);
         o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[i], o[d], 0, 0, 0);
       }
+      if (i % 4 == 3) hold_order();
     }
   }
   static __device__ __forceinline__ float elem(const void* base, size_t i) { return ((const float*)base)[i]; }
@@ -146,48 +167,60 @@ struct Rows {
   f16v o[4];
 };
 
-// One tile of 32 entries; `seen`: bit t is set if the lane's row sees entry t (0 where the slot holds none).  Slots that
-// hold nothing have zeros in V.
-template <int DT>
-__device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, const typename Mma<DT>::Q& q, uint32_t seen, float sc, int lane) {
-  const f16v s = Mma<DT>::qk(k, q, lane);
-  const uint32_t mine = seen >> (4 * (lane >> 5));
-  float x[16], mx = -__builtin_inff();
+// N tiles of 32 entries; full: every row sees all of them, else bit t of `seen` is set if the lane's row sees entry t (0 where the
+// slot holds none).  Slots that hold nothing have zeros in V.
+// The accumulators are rescaled only when a maximum has grown by more than 2^8 since they were last: until then weights grow up to 2^8,
+// which no type minds, and 64 products per tile and row are saved in all but a few tiles.
+constexpr float kLazy = 8.f;
+template <int DT, int N>
+__device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, const typename Mma<DT>::Q& q, bool full, unsigned long long seen, float sc, int lane) {
+  f16v s[N];
+  Mma<DT>::template qk<N>(s, k, q, lane);
+  if (!full) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    x[i] = (mine >> entry_of(i, 0)) & 1u ? s[i] * sc : -__builtin_inff();
-    mx = fmaxf(mx, x[i]);
+    for (int n = 0; n < N; ++n) {
+      const uint32_t mine = (uint32_t)(seen >> (32 * n)) >> (4 * (lane >> 5));
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[n][i] = (mine >> entry_of(i, 0)) & 1u ? s[n][i] : -__builtin_inff();
+    }
   }
+  float mx = -__builtin_inff();
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[n][i]);
   const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-  const float mn = fmaxf(st.m, fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])));
-  const float alpha = mn == st.m ? 1.f : __builtin_amdgcn_exp2f(st.m - mn);
-  st.m = mn;
-  st.l *= alpha;
+  mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * sc;
+  if (__any(mx > st.m + kLazy)) {                    // (from -inf: any finite one)
+    const float mn = fmaxf(st.m, mx), alpha = mn == st.m ? 1.f : __builtin_amdgcn_exp2f(st.m - mn);
+    st.m = mn;
+    st.l *= alpha;
 #pragma unroll
-  for (int d = 0; d < 4; ++d) st.o[d] *= alpha;
-  const float base = mn == -__builtin_inff() ? 0.f : mn;      // nothing seen yet
-  float p[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    p[i] = __builtin_amdgcn_exp2f(x[i] - base);
-    st.l += p[i];
+    for (int d = 0; d < 4; ++d) st.o[d] *= alpha;
   }
-  Mma<DT>::pv(st.o, v, p, lane);
+  const float base = st.m == -__builtin_inff() ? 0.f : -st.m;      // nothing seen yet
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    float p[16], sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], sc, base));
+      sum[i & 3] += p[i];
+    }
+    st.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    Mma<DT>::pv(st.o, v + n * kSub * Mma<DT>::kRowV, p, lane);
+  }
 }
 
 enum Source { kList, kPacked8, kPacked4 };
 
-struct Span { int splits, first, last; };            // tiles of 32 entries [first, last) of one split
 // How the L entries of a unit are shared: the same in the kernel that works and in the one that joins.
 __device__ __forceinline__ int splits_of(int L, int S, int chunk) { return min(S, max(1, L / chunk)); }
 
-// 16 bytes of tile row `row`, chunk c -> its place
-__device__ __forceinline__ char* place(char* tile, int rowb, int row, int c) { return tile + row * rowb + ((c ^ fz(row)) << 4); }
-
-// Writes the values of 16 or 32 codes (16 bytes) of one block, tile row `row`, chunk by chunk of the row.
+// Writes the values of 16 or 32 codes (16 bytes) of one block to `to`.
 template <int DT, int BITS>
-__device__ __forceinline__ void spread(char* tile, int row, int part, uint4 w4, float scale) {
-  constexpr int rowb = Mma<DT>::kRow, kVals = 128 / BITS, per = 16 / Mma<DT>::kES;   // values per chunk of the tile
+__device__ __forceinline__ void spread(char* to, uint4 w4, float scale) {
+  constexpr int kVals = 128 / BITS, per = 16 / Mma<DT>::kES;   // values per chunk of the tile
   const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
   for (int c = 0; c < kVals / per; ++c) {
@@ -203,24 +236,99 @@ __device__ __forceinline__ void spread(char* tile, int row, int part, uint4 w4, 
       for (int k = 0; k < 4; ++k) o[k] = __float_as_uint(x[k]);
     } else {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] = Mma<DT>::round16(x[2 * k]) | ((uint32_t)Mma<DT>::round16(x[2 * k + 1]) << 16);   // exact
+      for (int k = 0; k < 4; ++k) o[k] = Mma<DT>::round2(x[2 * k], x[2 * k + 1]);   // exact
     }
-    *(uint4*)place(tile, rowb, row, part * (kVals / per) + c) = uint4{o[0], o[1], o[2], o[3]};
+    *(uint4*)(to + 16 * c) = uint4{o[0], o[1], o[2], o[3]};
   }
 }
 
-// grid: XCD-interleaved (unit, split) x row blocks; 4 wavefronts, each with all its rows in registers and a tile of its own.
-template <int DT, int SRC>
-__global__ __launch_bounds__(256) void tree_kernel(TreeArgs a) {
+// What a wavefront holds of the tile that is on its way: N rows of 16-bit or float32 storage or of codes, K and V.
+// begin() requests rows r0 .. r0 + N - 1 of a tile, end() writes them to the tile in LDS, zeros in slots that hold nothing.
+template <int DT, int SRC, int N>
+struct Stage;
+
+template <int DT, int N>
+struct Stage<DT, kList, N> {
   using M = Mma<DT>;
-  constexpr int kTile = kSub * M::kRow, kOut = kHeadDim + 4;      // bytes of a K or V tile; floats of a row in the merge
+  static constexpr int kPer = 64 * 16 / M::kRow, kLoads = N / kPer;      // rows that 64 lanes load at once
+  uint4 k[kLoads], v[kLoads];
+  // ent: lane 4 e holds list entry e of the tile (-1: none)
+  __device__ __forceinline__ void begin(const TreeArgs& a, const char* pages, int ent, int r0, int lane) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      // an entry is four slots in a row; slots beyond its tokens and missing entries read slot 0 instead, of page 0
+      const int first = r0 + i * kPer, sub = lane * 16 / M::kRow, en = max(0, __builtin_amdgcn_readlane(ent, first & ~3));
+      const int slot = min((first & 3) + sub, en & 3);
+      const char* p = pages + (size_t)(en >> 4) * (kPageElems * M::kES) + ((en >> 2) & 3) * 4 * M::kRow + slot * M::kRow + lane % (M::kRow / 16) * 16;
+      k[i] = *(const uint4*)p;
+      v[i] = *(const uint4*)(p + 2048 * M::kES);
+    }
+  }
+  __device__ __forceinline__ void end(char* kt, char* vt, unsigned long long seen, bool full, int r0, int lane) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = r0 + i * kPer + lane * 16 / M::kRow, c = lane % (M::kRow / 16) * 16;
+      if (!full && !((seen >> r) & 1u)) { k[i] = uint4{0, 0, 0, 0}; v[i] = uint4{0, 0, 0, 0}; }
+      *(uint4*)(kt + r * M::kRowK + c) = k[i];
+      *(uint4*)(vt + r * M::kRowV + c) = v[i];
+    }
+  }
+};
+
+template <int DT, int BITS, int N>
+struct StagePacked {
+  static constexpr int kBytes = kHeadDim * BITS / 8, kParts = kBytes / 16, kLoads = N * kParts / 64;
+  uint4 k[kLoads], v[kLoads];
+  uint32_t ks[kLoads], vs[kLoads];
+  // rows first + r of the cache; beyond `left` rows the last one instead
+  __device__ __forceinline__ void begin(const TreeArgs& a, size_t first, int left, int r0, int lane) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = min(r0 + (i * 64 + lane) / kParts, left - 1), part = lane % kParts;
+      const size_t row = first + r;
+      k[i] = *(const uint4*)((const char*)a.cache.k_codes + row * kBytes + part * 16);
+      v[i] = *(const uint4*)((const char*)a.cache.v_codes + row * kBytes + part * 16);
+      ks[i] = a.cache.k_scales[row * kRowScales + part * 4 / kParts];
+      vs[i] = a.cache.v_scales[row * kRowScales + part * 4 / kParts];
+    }
+  }
+  __device__ __forceinline__ void end(char* kt, char* vt, int left, int r0, int lane) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = r0 + (i * 64 + lane) / kParts, part = lane % kParts;
+      const bool ok = r < left;
+      constexpr int wide = Mma<DT>::kRow / kParts;   // bytes of the values of a part
+      spread<DT, BITS>(kt + r * Mma<DT>::kRowK + part * wide, ok ? k[i] : uint4{0, 0, 0, 0}, ok ? scale_value(ks[i]) : 0.f);
+      spread<DT, BITS>(vt + r * Mma<DT>::kRowV + part * wide, ok ? v[i] : uint4{0, 0, 0, 0}, ok ? scale_value(vs[i]) : 0.f);
+    }
+  }
+};
+template <int DT, int N> struct Stage<DT, kPacked8, N> : StagePacked<DT, 8, N> {};
+template <int DT, int N> struct Stage<DT, kPacked4, N> : StagePacked<DT, 4, N> {};
+
+// grid: XCD-interleaved (unit, split) x row blocks.  Four wavefronts: WR of them take 32 rows each and share tiles of kSlots entries,
+// 4 / WR such groups take the split's tiles in turn.  The next tile is on its way in registers while one is consumed.
+template <int DT, int SRC, int WR>
+struct Shape {
+  static constexpr int kGroups = 4 / WR, kSlots = WR == 1 ? kSub : 2 * kSub, kMine = kSlots / WR;   // rows of a tile that a wavefront loads
+  static constexpr int kTileK = kSlots * Mma<DT>::kRowK, kTile = kTileK + kSlots * Mma<DT>::kRowV;     // bytes
+  static constexpr int kOut = kHeadDim + 4;                                                         // floats of a row in the merge
+  static constexpr int kMerge = 4 * kSub * kOut * 4, kTiles = kGroups * kTile, kLds = kTiles > kMerge ? kTiles : kMerge;
+};
+
+template <int DT, int SRC, int WR>
+__global__ __launch_bounds__(256, DT == DYNAKV_F32 ? 1 : 2) void tree_kernel(TreeArgs a) {
+  using M = Mma<DT>;
+  using Sh = Shape<DT, SRC, WR>;
+  constexpr int kOut = Sh::kOut, kSlots = Sh::kSlots, N = kSlots / kSub;
   extern __shared__ __align__(16) char lds[];
   // workgroups with the same entries run on the same XCD, one after the other: they share its L2
   const int us = ((int)blockIdx.x >> 3) / a.RB * 8 + ((int)blockIdx.x & 7), rb = ((int)blockIdx.x >> 3) % a.RB;
   if (us >= a.U * a.S) return;
   const int u = us / a.S, s = us % a.S;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-  const int R = a.T * a.G, row = rb * kSub + (lane & 31);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const int grp = wave / WR, wr = wave % WR;
+  const int R = a.T * a.G, row0 = (rb * WR + wr) * kSub, row = row0 + (lane & 31);
   const bool live = row < R;
 
   int L, nlist = 0;
@@ -232,7 +340,7 @@ __global__ __launch_bounds__(256) void tree_kernel(TreeArgs a) {
   }
   const int ns = splits_of(L, a.S, a.chunk);
   if (s >= ns) return;
-  const int nt = (L + kSub - 1) / kSub, t0 = (int)((long long)nt * s / ns), t1 = (int)((long long)nt * (s + 1) / ns);
+  const int nt = (L + kSlots - 1) / kSlots, t0 = (int)((long long)nt * s / ns), t1 = (int)((long long)nt * (s + 1) / ns);
 
   typename M::Q q;
   M::load_q(q, a.Q, (size_t)u * R + (live ? row : 0), h, live);
@@ -240,104 +348,112 @@ __global__ __launch_bounds__(256) void tree_kernel(TreeArgs a) {
   st.m = -__builtin_inff(); st.l = 0.f;
 #pragma unroll
   for (int d = 0; d < 4; ++d) st.o[d] = f16v{};
-  char* kt = lds + wave * 2 * kTile;
-  char* vt = kt + kTile;
+  char* kt = lds + grp * Sh::kTile;
+  char* vt = kt + Sh::kTileK;
 
-  for (int t = t0 + wave; t < t1; t += 4) {
-    uint32_t seen;
-    if constexpr (SRC == kList) {
-      constexpr int kPer = 64 * 16 / M::kRow;        // rows that 64 lanes load at once
-      const char* pages = a.pages + (size_t)u * a.unit_pages;
-      const int e = 8 * t + (lane >> 2 & 7);
-      const int ent = e < nlist ? a.plist[(size_t)u * a.Lcap + e] : -1;
-      seen = (uint32_t)__ballot(ent >= 0 && (lane & 3) <= (ent & 3));
-#pragma unroll
-      for (int i = 0; i < kSub / kPer; ++i) {
-        const int r = i * kPer + lane * 16 / M::kRow, c = lane % (M::kRow / 16), en = __shfl(ent, r & ~3);
-        uint4 kk = {0, 0, 0, 0}, vv = {0, 0, 0, 0};
-        if ((seen >> r) & 1u) {
-          const char* p = pages + (size_t)(en >> 4) * (kPageElems * M::kES) + (((en >> 2) & 3) * 4 + (r & 3)) * M::kRow + c * 16;
-          kk = *(const uint4*)p;
-          vv = *(const uint4*)(p + 2048 * M::kES);
-        }
-        *(uint4*)place(kt, M::kRow, r, c) = kk;
-        *(uint4*)place(vt, M::kRow, r, c) = vv;
-      }
-    } else {
-      constexpr int bits = SRC == kPacked8 ? 8 : 4, cb = kHeadDim * bits / 8, parts = cb / 16;
-      const int n = min(kSub, L - t * kSub);
-      seen = n >= kSub ? ~0u : (1u << n) - 1u;
-      const size_t first = (size_t)u * a.cache.capacity + (size_t)t * kSub;
-#pragma unroll
-      for (int i = 0; i < kSub * parts / 64; ++i) {
-        const int r = (i * 64 + lane) / parts, part = lane % parts;
-        uint4 kk = {0, 0, 0, 0}, vv = {0, 0, 0, 0};
-        uint32_t ks = 127, vs = 127;
-        if (r < n) {
-          kk = *(const uint4*)((const char*)a.cache.k_codes + (first + r) * cb + part * 16);
-          vv = *(const uint4*)((const char*)a.cache.v_codes + (first + r) * cb + part * 16);
-          ks = a.cache.k_scales[(first + r) * kRowScales + part * 4 / parts];
-          vs = a.cache.v_scales[(first + r) * kRowScales + part * 4 / parts];
-        }
-        spread<DT, bits>(kt, r, part, kk, scale_value(ks));
-        spread<DT, bits>(vt, r, part, vv, scale_value(vs));
+  // a wavefront's own tile needs no barrier: its LDS operations keep their order, and so must the compiler
+  auto sync = [] {
+    if constexpr (WR == 1) asm volatile("" ::: "memory");
+    else lds_barrier();
+  };
+  const char* pages = a.pages + (size_t)u * a.unit_pages;
+  const int* plist = a.plist + (size_t)u * a.Lcap;
+  const size_t first = (size_t)u * a.cache.capacity;
+  auto entry = [&](int t) {                          // list entry (lane / 4) of tile t
+    const int e = t * (kSlots / 4) + (lane >> 2) % (kSlots / 4);
+    return t < t1 && e < nlist ? plist[e] : -1;
+  };
+  Stage<DT, SRC, Sh::kMine> stage;
+  const int r0 = wr * Sh::kMine;
+  int t = t0 + grp, ent = -1, ent_next = -1;
+  if constexpr (SRC == kList) { ent = entry(t); ent_next = entry(t + Sh::kGroups); }
+  auto begin = [&](int tile, int e) {
+    if constexpr (SRC == kList) stage.begin(a, pages, e, r0, lane);
+    else stage.begin(a, first + (size_t)tile * kSlots, L - tile * kSlots, r0, lane);
+  };
+  if (t < t1) begin(t, ent);
+  const int rounds = (t1 - t0 + Sh::kGroups - 1) / Sh::kGroups;      // of the whole workgroup: barriers are common
+  for (int i = 0; i < rounds; ++i, t += Sh::kGroups) {
+    constexpr unsigned long long kAll = kSlots == 64 ? ~0ull : 0xFFFFFFFFull;
+    const bool have = t < t1;
+    unsigned long long seen = 0;
+    if (have) {
+      if constexpr (SRC == kList) {
+        seen = __ballot(ent >= 0 && (lane & 3) <= (ent & 3)) & kAll;
+        stage.end(kt, vt, seen, seen == kAll, r0, lane);
+      } else {
+        const int left = L - t * kSlots;
+        seen = left >= kSlots ? kAll : (1ull << left) - 1;
+        stage.end(kt, vt, left, r0, lane);
       }
     }
-    asm volatile("" ::: "memory");                   // the same wavefront's LDS operations keep their order; the compiler must too
-    consume<DT>(st, kt, vt, q, seen, a.sc, lane);
-    asm volatile("" ::: "memory");
+    sync();
+    if (t + Sh::kGroups < t1) {
+      begin(t + Sh::kGroups, ent_next);
+      if constexpr (SRC == kList) { ent = ent_next; ent_next = entry(t + 2 * Sh::kGroups); }
+    }
+    if (have) consume<DT, N>(st, kt, vt, q, seen == kAll, seen, a.sc, lane);
+    sync();
   }
 
-  // the drafted tokens: the unit's last split, one tile of 32 per wavefront
-  if (s == ns - 1 && a.K1 && wave * kSub < a.T) {
-    constexpr int kPer = 64 * 16 / M::kRow;
-    const int j0 = wave * kSub;
-    uint32_t bad = 0;
+  // the drafted tokens: the unit's last split, tiles of 32, one for each of the first groups
+  const int j0 = grp * kSub;
+  if (s == ns - 1 && a.K1) {
+    constexpr int kPer = 64 * 16 / M::kRow, kTrees = Sh::kGroups >= 2 ? 1 : 2;
+    for (int w = 0; w < kTrees; ++w) {               // (a single group takes both)
+      const int j1 = j0 + w * kSub;
+      uint32_t bad = 0;
+      if (j1 < a.T) {
+#pragma unroll 2
+        for (int i = 0; i < kSub / kPer; ++i) {      // every wavefront of the group writes the same: they need not wait for each other
+          const int r = i * kPer + lane * 16 / M::kRow, c = lane % (M::kRow / 16) * 16;
+          uint4 kk = {0, 0, 0, 0}, vv = {0, 0, 0, 0};
+          bool b = false;
+          if (j1 + r < a.T) {
+            const size_t at = ((size_t)u * a.T + j1 + r) * M::kRow + c;
+            kk = *(const uint4*)((const char*)a.K1 + at);
+            vv = M::only_finite(*(const uint4*)((const char*)a.V1 + at), b);
+          }
+          *(uint4*)(kt + r * M::kRowK + c) = kk;
+          *(uint4*)(vt + r * M::kRowV + c) = vv;
+          const unsigned long long any = __ballot(b);
 #pragma unroll
-    for (int i = 0; i < kSub / kPer; ++i) {
-      const int r = i * kPer + lane * 16 / M::kRow, c = lane % (M::kRow / 16);
-      uint4 kk = {0, 0, 0, 0}, vv = {0, 0, 0, 0};
-      bool b = false;
-      if (j0 + r < a.T) {
-        const size_t at = ((size_t)u * a.T + j0 + r) * M::kRow + c * 16;
-        kk = *(const uint4*)((const char*)a.K1 + at);
-        vv = M::only_finite(*(const uint4*)((const char*)a.V1 + at), b);
-      }
-      *(uint4*)place(kt, M::kRow, r, c) = kk;
-      *(uint4*)place(vt, M::kRow, r, c) = vv;
-      const unsigned long long any = __ballot(b);
-#pragma unroll
-      for (int z = 0; z < kPer; ++z)
-        if ((any >> (z * (64 / kPer))) & (~0ull >> (64 - 64 / kPer))) bad |= 1u << (i * kPer + z);
-    }
-    const int node = (live ? row : 0) / a.G;
-    unsigned long long bits = a.tree ? a.tree[(size_t)u * a.T + node] : ~0ull >> (63 - node);
-    if (a.T < 64) bits &= (1ull << a.T) - 1;
-    const uint32_t seen = (uint32_t)(bits >> j0);
-    asm volatile("" ::: "memory");
-    consume<DT>(st, kt, vt, q, seen, a.sc, lane);
-    asm volatile("" ::: "memory");
-    // values that are not finite went in as zeros, so that a row which does not see their token stays clean of them; the
-    // rows that see it get them here
-    while (bad) {
-      const int j = __builtin_ctz(bad);
-      bad &= bad - 1;
-      const bool sees = (seen >> j) & 1u;
-      const size_t at = ((size_t)u * a.T + j0 + j) * kHeadDim;
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float x = M::elem(a.V1, at + 32 * d + entry_of(i, 0) + 4 * h);
-          if (sees && !(fabsf(x) < __builtin_inff())) st.o[d][i] += x;
+          for (int z = 0; z < kPer; ++z)
+            if ((any >> (z * (64 / kPer))) & (~0ull >> (64 - 64 / kPer))) bad |= 1u << (i * kPer + z);
         }
+      }
+      sync();
+      if (j1 < a.T) {
+        const int node = (live ? row : 0) / a.G;
+        unsigned long long bits = a.tree ? a.tree[(size_t)u * a.T + node] : ~0ull >> (63 - node);
+        if (a.T < 64) bits &= (1ull << a.T) - 1;
+        const uint32_t seen = (uint32_t)(bits >> j1);
+        consume<DT, 1>(st, kt, vt, q, false, seen, a.sc, lane);
+        // values that are not finite went in as zeros, so that a row which does not see their token stays clean of them;
+        // the rows that see it get them here
+        while (bad) {
+          const int j = __builtin_ctz(bad);
+          bad &= bad - 1;
+          const bool sees = (seen >> j) & 1u;
+          const size_t at = ((size_t)u * a.T + j1 + j) * kHeadDim;
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float x = M::elem(a.V1, at + 32 * d + entry_of(i, 0) + 4 * h);
+              if (sees && !(fabsf(x) < __builtin_inff())) st.o[d][i] += x;
+              if (i % 8 == 7) hold_order();
+            }
+        }
+      }
+      sync();
     }
   }
 
-  // join the four wavefronts: every one leaves its rows in LDS
+  // join the groups: every wavefront leaves its rows in LDS
   const auto lsum = __builtin_amdgcn_permlane32_swap(__float_as_uint(st.l), __float_as_uint(st.l), false, false);
   st.l = __uint_as_float(lsum[0]) + __uint_as_float(lsum[1]);
-  __syncthreads();
+  lds_barrier();
   float* mo = (float*)lds;
   {
     float* mine = mo + ((size_t)wave * kSub + (lane & 31)) * kOut;
@@ -347,19 +463,19 @@ __global__ __launch_bounds__(256) void tree_kernel(TreeArgs a) {
       for (int i = 0; i < 16; i += 4) *(f4*)(mine + 32 * d + entry_of(i, h)) = f4{st.o[d][i], st.o[d][i + 1], st.o[d][i + 2], st.o[d][i + 3]};
     if (h == 0) { mine[kHeadDim] = st.m; mine[kHeadDim + 1] = st.l; }
   }
-  __syncthreads();
-  for (int t = threadIdx.x; t < kSub * (kHeadDim / 4); t += 256) {
-    const int r = t >> 5, c = (t & 31) * 4, rr = rb * kSub + r;
+  lds_barrier();
+  for (int i = threadIdx.x; i < WR * kSub * (kHeadDim / 4); i += 256) {
+    const int r = i >> 5, c = (i & 31) * 4, rr = rb * WR * kSub + r;      // row r of the workgroup: wavefront r / 32 of every group
     if (rr >= R) break;
-    float mw[4], m = -__builtin_inff(), l = 0.f;
+    float mw[Sh::kGroups], m = -__builtin_inff(), l = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) { mw[w] = mo[(w * kSub + r) * kOut + kHeadDim]; m = fmaxf(m, mw[w]); }
+    for (int w = 0; w < Sh::kGroups; ++w) { mw[w] = mo[(w * WR * kSub + r) * kOut + kHeadDim]; m = fmaxf(m, mw[w]); }
     f4 o = {0, 0, 0, 0};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < Sh::kGroups; ++w) {
       if (mw[w] == -__builtin_inff()) continue;       // that wavefront saw nothing of this row
       const float f = mw[w] == m ? 1.f : __builtin_amdgcn_exp2f(mw[w] - m);
-      const float* x = mo + (w * kSub + r) * kOut;
+      const float* x = mo + (w * WR * kSub + r) * kOut;
       l += f * x[kHeadDim + 1];
       o += f * *(const f4*)(x + c);
     }
@@ -403,34 +519,44 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   if (a.lse && c == 0) a.lse[i] = none ? m : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+// Wavefronts of a workgroup that take rows of their own, up to four times 32 of the R rows of a unit.
+int row_waves(int dtype, int R) { return dtype == DYNAKV_F32 || R <= kSub ? 1 : R <= 2 * kSub ? 2 : 4; }
 // Workgroups that may share a unit's entries, so that about two workgroups per compute unit have work.
-int most_splits(int U, int R) {
-  const long long wgs = (long long)U * ((R + kSub - 1) / kSub);
+int most_splits(int dtype, int U, int R) {
+  const int rows = row_waves(dtype, R) * kSub;
+  const long long wgs = (long long)U * ((R + rows - 1) / rows);
   const long long s = (512 + wgs - 1) / wgs;
   return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+}
+
+template <int DT, int SRC, int WR>
+hipError_t launch_shape(TreeArgs& a, hipStream_t st) {
+  using Sh = Shape<DT, SRC, WR>;
+  const int R = a.T * a.G;
+  a.RB = (R + WR * kSub - 1) / (WR * kSub);
+  const long long us = ((long long)a.U * a.S + 7) / 8 * 8;
+  tree_kernel<DT, SRC, WR><<<(unsigned)(us * a.RB), 256, Sh::kLds, st>>>(a);
+  return hipGetLastError();
+}
+
+template <int DT, int SRC>
+hipError_t launch_source(TreeArgs& a, hipStream_t st) {
+  if constexpr (DT == DYNAKV_F32) {
+    return launch_shape<DT, SRC, 1>(a, st);
+  } else {
+    const int wr = row_waves(DT, a.T * a.G);
+    return wr == 1 ? launch_shape<DT, SRC, 1>(a, st) : wr == 2 ? launch_shape<DT, SRC, 2>(a, st) : launch_shape<DT, SRC, 4>(a, st);
+  }
 }
 
 template <int DT>
 hipError_t launch(TreeArgs a, hipStream_t st) {
   const int R = a.T * a.G;
-  a.RB = (R + kSub - 1) / kSub;
-  a.S = most_splits(a.U, R);
+  a.S = most_splits(DT, a.U, R);
   // a partial result costs a row 2 * 528 bytes of traffic: a workgroup's share of the entries is several times that
-  a.chunk = max(256, 4 * R);
+  a.chunk = R < 64 ? 256 : 4 * R;
   while (a.S > 1 && (long long)a.chunk * (a.S - 1) >= a.most) --a.S;
-  const long long us = ((long long)a.U * a.S + 7) / 8 * 8;
-  const unsigned grid = (unsigned)(us * a.RB);
-  const size_t tiles = 4 * 2 * kSub * Mma<DT>::kRow, merge = 4 * kSub * (kHeadDim + 4) * 4, lds = tiles > merge ? tiles : merge;
-  const void* f;
-  if (a.pages) f = (const void*)tree_kernel<DT, kList>;
-  else if (a.cache.bits == 8) f = (const void*)tree_kernel<DT, kPacked8>;
-  else f = (const void*)tree_kernel<DT, kPacked4>;
-  if (lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-  }
-  void* args[] = {&a};
-  const hipError_t e = hipLaunchKernel(f, dim3(grid), dim3(256), args, lds, st);
+  const hipError_t e = a.pages ? launch_source<DT, kList>(a, st) : a.cache.bits == 8 ? launch_source<DT, kPacked8>(a, st) : launch_source<DT, kPacked4>(a, st);
   if (e != hipSuccess) return e;
   if (a.S > 1) tree_join_kernel<DT><<<(unsigned)(((long long)a.U * R + 7) / 8), 256, 0, st>>>(a);
   return hipGetLastError();
@@ -440,7 +566,7 @@ hipError_t launch(TreeArgs a, hipStream_t st) {
 
 size_t tree_scratch_bytes(int U, int T, int G) {
   const size_t R = (size_t)T * G;
-  const int S = most_splits(U, (int)R);
+  const int s16 = most_splits(DYNAKV_F16, U, (int)R), s32 = most_splits(DYNAKV_F32, U, (int)R), S = s16 > s32 ? s16 : s32;
   return 256 + (S > 1 ? (size_t)U * S * R * kPartRow * sizeof(float) : 0);
 }
 
