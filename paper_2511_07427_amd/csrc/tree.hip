@@ -51,17 +51,25 @@ struct Mma {
     else
       return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
   }
-  // scores of N tiles of 32 entries each, kSub rows apart
+  // Scores of N tiles of 32 entries each, kSub rows apart.  The operands of a step are requested two steps before it.
   template <int N>
   static __device__ __forceinline__ void qk(f16v (&c)[N], const char* k, const Q& q, int lane) {
     const char* at = k + (lane & 31) * kRowK + (lane >> 5) * 16;
+    uint4 f[8][N];
+    auto request = [&](int s) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) f[s][n] = *(const uint4*)(at + n * kSub * kRowK + s * 32);
+    };
 #pragma unroll
     for (int n = 0; n < N; ++n) c[n] = f16v{};
+    request(0);
+    request(1);
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
+      if (s + 2 < 8) request(s + 2);
+      hold_order();
 #pragma unroll
-      for (int n = 0; n < N; ++n) c[n] = mma(*(const uint4*)(at + n * kSub * kRowK + s * 32), q.b[s], c[n]);
-      if (s % 4 == 3) hold_order();
+      for (int n = 0; n < N; ++n) c[n] = mma(f[s][n], q.b[s], c[n]);
     }
   }
   static __device__ __forceinline__ uint16_t round16(float x) {
@@ -72,28 +80,19 @@ struct Mma {
     if constexpr (DT == DYNAKV_BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2v){x, y}, b2));
     else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2v){x, y}, h2));
   }
-  static __device__ __forceinline__ void pv(f16v (&o)[4], const char* v, const float (&p)[16], int lane) {
-    // a group of 16 lanes reads 4 entries (rows) of 16 columns and gets the 4 entries of one column per lane
+  // V^T of the 16 entries of chunk c: a group of 16 lanes reads 4 entries (rows) of 16 columns and gets the 4 entries of one column
+  // per lane
+  struct VFrag { uint4 d[4]; };
+  static __device__ __forceinline__ void load_v(VFrag& f, const char* v, int c, int lane) {
     const int j = lane & 15;
-    const char* from = v + ((lane >> 5) * 4 + (j >> 2)) * kRowV + ((lane >> 4) & 1) * 32 + (j & 3) * 8;
+    const char* from = v + ((lane >> 5) * 4 + (j >> 2)) * kRowV + ((lane >> 4) & 1) * 32 + (j & 3) * 8 + c * 16 * kRowV;
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      // the probability that weights V goes in rounded to V's type: an error of half a step relative to each term, as much
-      // as rounding the output costs
-      uint32_t w[4];
+    for (int d = 0; d < 4; ++d) {
+      uint2 a[2];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) w[k] = round2(p[8 * c + 2 * k], p[8 * c + 2 * k + 1]);
-      const uint4 b = {w[0], w[1], w[2], w[3]};
-#pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        uint2 a[2];
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-          a[x] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                               (__attribute__((address_space(3))) s4*)(from + (16 * c + 8 * x) * kRowV + d * 64)));
-        o[d] = mma(uint4{a[0].x, a[0].y, a[1].x, a[1].y}, b, o[d]);
-      }
-      hold_order();
+      for (int x = 0; x < 2; ++x)
+        a[x] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)(from + 8 * x * kRowV + d * 64)));
+      f.d[d] = uint4{a[0].x, a[0].y, a[1].x, a[1].y};
     }
   }
   static __device__ __forceinline__ float elem(const void* base, size_t i) { return load_elem(base, i, DT); }
@@ -116,6 +115,7 @@ struct Mma {
 
 template <>
 struct Mma<DYNAKV_F32> {
+  struct VFrag {};
   static constexpr int kES = 4, kRow = kHeadDim * 4, kRowK = kRow + 16, kRowV = kRow + 32;
   struct Q { f4 b[16]; };
   static __device__ __forceinline__ void load_q(Q& q, const void* base, size_t row, int h, bool ok) {
@@ -173,15 +173,30 @@ struct Rows {
 // which no type minds, and 64 products per tile and row are saved in all but a few tiles.
 constexpr float kLazy = 8.f;
 template <int DT, int N>
-__device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, const typename Mma<DT>::Q& q, bool full, unsigned long long seen, float sc, int lane) {
+__device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, const typename Mma<DT>::Q& q, bool full, bool alike, unsigned long long seen, float sc,
+                                        int lane) {
+  using M = Mma<DT>;
   f16v s[N];
-  Mma<DT>::template qk<N>(s, k, q, lane);
+  M::template qk<N>(s, k, q, lane);
+  [[maybe_unused]] typename M::VFrag f[2];
+  if constexpr (DT != DYNAKV_F32) M::load_v(f[0], v, 0, lane);       // arrives while the maxima are taken
   if (!full) {
+    if (alike) {                                     // the same slots for every row: the conditions are scalars
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const uint32_t mine = (uint32_t)(seen >> (32 * n)) >> (4 * (lane >> 5));
+      for (int n = 0; n < N; ++n)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[n][i] = (mine >> entry_of(i, 0)) & 1u ? s[n][i] : -__builtin_inff();
+        for (int i = 0; i < 16; ++i) {
+          const int e = 32 * n + entry_of(i, 0);
+          const unsigned long long lo = (seen >> e) & 1 ? 0xFFFFFFFFull : 0, hi = (seen >> (e + 4)) & 1 ? 0xFFFFFFFF00000000ull : 0;
+          s[n][i] = __builtin_amdgcn_inverse_ballot_w64(lo | hi) ? s[n][i] : -__builtin_inff();
+        }
+    } else {
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const uint32_t mine = (uint32_t)(seen >> (32 * n)) >> (4 * (lane >> 5));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[n][i] = (mine >> entry_of(i, 0)) & 1u ? s[n][i] : -__builtin_inff();
+      }
     }
   }
   float mx = -__builtin_inff();
@@ -199,16 +214,40 @@ __device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, 
     for (int d = 0; d < 4; ++d) st.o[d] *= alpha;
   }
   const float base = st.m == -__builtin_inff() ? 0.f : -st.m;      // nothing seen yet
+  if constexpr (DT == DYNAKV_F32) {
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    float p[16], sum[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int n = 0; n < N; ++n) {
+      float p[16], sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], sc, base));
-      sum[i & 3] += p[i];
+      for (int i = 0; i < 16; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], sc, base));
+        sum[i & 3] += p[i];
+      }
+      st.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      M::pv(st.o, v + n * kSub * M::kRowV, p, lane);
     }
-    st.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    Mma<DT>::pv(st.o, v + n * kSub * Mma<DT>::kRowV, p, lane);
+  } else {
+    // 16 entries at a time: while the matrix cores take one chunk, the next one's weights are computed and its V is on its way.
+    // A weight goes in rounded to V's type: an error of half a step relative to each term, as much as rounding the output costs.
+    auto weights = [&](int c) {
+      float p[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[c >> 1][8 * (c & 1) + i], sc, base));
+      st.l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      return uint4{M::round2(p[0], p[1]), M::round2(p[2], p[3]), M::round2(p[4], p[5]), M::round2(p[6], p[7])};
+    };
+    uint4 w = weights(0);
+#pragma unroll
+    for (int c = 0; c < 2 * N; ++c) {
+      if (c + 1 < 2 * N) M::load_v(f[(c + 1) & 1], v, c + 1, lane);
+      hold_order();
+      uint4 next = {};
+      if (c + 1 < 2 * N) next = weights(c + 1);
+#pragma unroll
+      for (int d = 0; d < 4; ++d) st.o[d] = M::mma(f[c & 1].d[d], w, st.o[d]);
+      w = next;
+      hold_order();
+    }
   }
 }
 
@@ -310,7 +349,7 @@ template <int DT, int N> struct Stage<DT, kPacked4, N> : StagePacked<DT, 4, N> {
 // 4 / WR such groups take the split's tiles in turn.  The next tile is on its way in registers while one is consumed.
 template <int DT, int SRC, int WR>
 struct Shape {
-  static constexpr int kGroups = 4 / WR, kSlots = WR == 1 ? kSub : 2 * kSub, kMine = kSlots / WR;   // rows of a tile that a wavefront loads
+  static constexpr int kGroups = 4 / WR, kSlots = WR == 4 ? 2 * kSub : kSub, kMine = kSlots / WR;   // rows of a tile that a wavefront loads
   static constexpr int kTileK = kSlots * Mma<DT>::kRowK, kTile = kTileK + kSlots * Mma<DT>::kRowV;     // bytes
   static constexpr int kOut = kHeadDim + 4;                                                         // floats of a row in the merge
   static constexpr int kMerge = 4 * kSub * kOut * 4, kTiles = kGroups * kTile, kLds = kTiles > kMerge ? kTiles : kMerge;
@@ -325,7 +364,7 @@ __global__ __launch_bounds__(256, DT == DYNAKV_F32 ? 1 : 2) void tree_kernel(Tre
   // workgroups with the same entries run on the same XCD, one after the other: they share its L2
   const int us = ((int)blockIdx.x >> 3) / a.RB * 8 + ((int)blockIdx.x & 7), rb = ((int)blockIdx.x >> 3) % a.RB;
   if (us >= a.U * a.S) return;
-  const int u = us / a.S, s = us % a.S;
+  const int u = us % a.U, s = us / a.U;              // units first: where a unit has fewer splits, all XCDs lack some
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int grp = wave / WR, wr = wave % WR;
   const int R = a.T * a.G, row0 = (rb * WR + wr) * kSub, row = row0 + (lane & 31);
@@ -359,40 +398,45 @@ __global__ __launch_bounds__(256, DT == DYNAKV_F32 ? 1 : 2) void tree_kernel(Tre
   const char* pages = a.pages + (size_t)u * a.unit_pages;
   const int* plist = a.plist + (size_t)u * a.Lcap;
   const size_t first = (size_t)u * a.cache.capacity;
-  auto entry = [&](int t) {                          // list entry (lane / 4) of tile t
-    const int e = t * (kSlots / 4) + (lane >> 2) % (kSlots / 4);
-    return t < t1 && e < nlist ? plist[e] : -1;
-  };
+  // List entry lane / 4 of tile t.  It is requested one tile before the tile's rows are, so that neither waits for the other, and looked
+  // at only there: a conditional load here, or a copy of what is on its way, would wait for every load before it.
+  auto entry_index = [&](int t) { return t * (kSlots / 4) + (lane >> 2) % (kSlots / 4); };
   Stage<DT, SRC, Sh::kMine> stage;
   const int r0 = wr * Sh::kMine;
-  int t = t0 + grp, ent = -1, ent_next = -1;
-  if constexpr (SRC == kList) { ent = entry(t); ent_next = entry(t + Sh::kGroups); }
-  auto begin = [&](int tile, int e) {
-    if constexpr (SRC == kList) stage.begin(a, pages, e, r0, lane);
-    else stage.begin(a, first + (size_t)tile * kSlots, L - tile * kSlots, r0, lane);
+  constexpr unsigned long long kAll = kSlots == 64 ? ~0ull : 0xFFFFFFFFull;
+  int t = t0 + grp, entry = 0;
+  unsigned long long seen = 0, seen_next = 0;        // slots of the tile that hold an entry
+  auto request_entry = [&](int tile) {
+    if constexpr (SRC == kList) entry = plist[min(entry_index(tile), nlist - 1)];
   };
-  if (t < t1) begin(t, ent);
+  auto begin = [&](int tile) {
+    if constexpr (SRC == kList) {
+      const int e = entry_index(tile) < nlist ? entry : -1;
+      seen_next = __ballot(e >= 0 && (lane & 3) <= (e & 3)) & kAll;
+      stage.begin(a, pages, e, r0, lane);
+      request_entry(tile + Sh::kGroups);
+    } else {
+      const int left = L - tile * kSlots;
+      seen_next = left >= kSlots ? kAll : (1ull << left) - 1;
+      stage.begin(a, first + (size_t)tile * kSlots, left, r0, lane);
+    }
+  };
+  if (t < t1) {
+    request_entry(t);
+    begin(t);
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0): the queries are there, and no iteration waits for them with the tile on its way
   const int rounds = (t1 - t0 + Sh::kGroups - 1) / Sh::kGroups;      // of the whole workgroup: barriers are common
   for (int i = 0; i < rounds; ++i, t += Sh::kGroups) {
-    constexpr unsigned long long kAll = kSlots == 64 ? ~0ull : 0xFFFFFFFFull;
     const bool have = t < t1;
-    unsigned long long seen = 0;
+    seen = seen_next;
     if (have) {
-      if constexpr (SRC == kList) {
-        seen = __ballot(ent >= 0 && (lane & 3) <= (ent & 3)) & kAll;
-        stage.end(kt, vt, seen, seen == kAll, r0, lane);
-      } else {
-        const int left = L - t * kSlots;
-        seen = left >= kSlots ? kAll : (1ull << left) - 1;
-        stage.end(kt, vt, left, r0, lane);
-      }
+      if constexpr (SRC == kList) stage.end(kt, vt, seen, seen == kAll, r0, lane);
+      else stage.end(kt, vt, L - t * kSlots, r0, lane);
     }
     sync();
-    if (t + Sh::kGroups < t1) {
-      begin(t + Sh::kGroups, ent_next);
-      if constexpr (SRC == kList) { ent = ent_next; ent_next = entry(t + 2 * Sh::kGroups); }
-    }
-    if (have) consume<DT, N>(st, kt, vt, q, seen == kAll, seen, a.sc, lane);
+    if (t + Sh::kGroups < t1) begin(t + Sh::kGroups);
+    if (have) consume<DT, N>(st, kt, vt, q, seen == kAll, true, seen, a.sc, lane);
     sync();
   }
 
@@ -428,7 +472,7 @@ __global__ __launch_bounds__(256, DT == DYNAKV_F32 ? 1 : 2) void tree_kernel(Tre
         unsigned long long bits = a.tree ? a.tree[(size_t)u * a.T + node] : ~0ull >> (63 - node);
         if (a.T < 64) bits &= (1ull << a.T) - 1;
         const uint32_t seen = (uint32_t)(bits >> j1);
-        consume<DT, 1>(st, kt, vt, q, false, seen, a.sc, lane);
+        consume<DT, 1>(st, kt, vt, q, false, false, seen, a.sc, lane);
         // values that are not finite went in as zeros, so that a row which does not see their token stays clean of them;
         // the rows that see it get them here
         while (bad) {
@@ -492,30 +536,53 @@ __global__ __launch_bounds__(256, DT == DYNAKV_F32 ? 1 : 2) void tree_kernel(Tre
   }
 }
 
-// Joins the splits of the units that have several: 32 lanes a row.
-template <int DT>
+// Joins the splits of the units that have several.  32 lanes take up to eight partial results of a row at once; of more, P = 8 such groups
+// share a row (64 partial results one after the other, each a trip to memory, took 52 us).
+template <int DT, int P>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
-  const int R = a.T * a.G;
-  const long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (i >= (long long)a.U * R) return;
-  const int u = (int)(i / R), r = (int)(i % R), c = (threadIdx.x & 31) * 4;
+  __shared__ __align__(16) float sm[8][kPartRow];
+  const int R = a.T * a.G, c = (threadIdx.x & 31) * 4, grp = threadIdx.x >> 5;
+  const size_t i = (size_t)blockIdx.x * (8 / P) + grp / P;
+  if (P < 8 && i >= (size_t)a.U * R) return;
+  const int u = (int)(i / R), r = (int)(i % R);
   const int L = a.pages ? 4 * a.n_list[u] : a.lengths ? min(max(a.lengths[u], 0), a.cache.capacity) : a.cache.capacity;
   const int ns = splits_of(L, a.S, a.chunk);
-  if (ns == 1) return;
+  if (ns == 1) return;                               // (P = 8: the whole workgroup)
   const float* p = a.part + ((size_t)u * a.S * R + r) * kPartRow;
-  float m = -__builtin_inff(), l = 0.f;
-  for (int s = 0; s < ns; ++s) m = fmaxf(m, p[(size_t)s * R * kPartRow + kHeadDim]);
-  f4 o = {0, 0, 0, 0};
-  for (int s = 0; s < ns; ++s) {
-    const float* x = p + (size_t)s * R * kPartRow;
-    const float ms = x[kHeadDim];
-    if (ms == -__builtin_inff()) continue;
-    const float f = ms == m ? 1.f : __builtin_amdgcn_exp2f(ms - m);
-    l += f * x[kHeadDim + 1];
-    o += f * *(const f4*)(x + c);
+  float ms[8], ls[8], m = -__builtin_inff(), l = 0.f;
+  f4 os[8], o = {0, 0, 0, 0};
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int s = grp % P + P * k;
+    const float* x = p + (size_t)min(s, ns - 1) * R * kPartRow;
+    ms[k] = s < ns ? x[kHeadDim] : -__builtin_inff();
+    ls[k] = x[kHeadDim + 1];
+    os[k] = *(const f4*)(x + c);
+  }
+  auto add = [&](float mk, float lk, const f4& ok) {
+    if (mk == -__builtin_inff()) return;             // saw nothing of this row, whatever its sums hold
+    const float f = mk == m ? 1.f : __builtin_amdgcn_exp2f(mk - m);
+    l += f * lk;
+    o += f * ok;
+  };
+#pragma unroll
+  for (int k = 0; k < 8; ++k) m = fmaxf(m, ms[k]);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) add(ms[k], ls[k], os[k]);
+  if constexpr (P == 8) {
+    *(f4*)&sm[grp][c] = o;
+    if (c == 0) { sm[grp][kHeadDim] = m; sm[grp][kHeadDim + 1] = l; }
+    __syncthreads();
+    if (grp > 0) return;
+    m = -__builtin_inff(); l = 0.f;
+    o = f4{0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m = fmaxf(m, sm[k][kHeadDim]);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) add(sm[k][kHeadDim], sm[k][kHeadDim + 1], *(const f4*)&sm[k][c]);
   }
   const bool none = m == -__builtin_inff();
-  Mma<DT>::store4(a.out, (size_t)i * kHeadDim + c, none ? f4{0, 0, 0, 0} : o / l);
+  Mma<DT>::store4(a.out, i * kHeadDim + c, none ? f4{0, 0, 0, 0} : o / l);
   if (a.lse && c == 0) a.lse[i] = none ? m : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
@@ -555,10 +622,11 @@ hipError_t launch(TreeArgs a, hipStream_t st) {
   a.S = most_splits(DT, a.U, R);
   // a partial result costs a row 2 * 528 bytes of traffic: a workgroup's share of the entries is several times that
   a.chunk = R < 64 ? 256 : 4 * R;
-  while (a.S > 1 && (long long)a.chunk * (a.S - 1) >= a.most) --a.S;
+  a.S = min(a.S, max(1, a.most / a.chunk));         // (more would have nothing to do)
   const hipError_t e = a.pages ? launch_source<DT, kList>(a, st) : a.cache.bits == 8 ? launch_source<DT, kPacked8>(a, st) : launch_source<DT, kPacked4>(a, st);
   if (e != hipSuccess) return e;
-  if (a.S > 1) tree_join_kernel<DT><<<(unsigned)(((long long)a.U * R + 7) / 8), 256, 0, st>>>(a);
+  if (a.S > 8) tree_join_kernel<DT, 8><<<(unsigned)((long long)a.U * R), 256, 0, st>>>(a);
+  else if (a.S > 1) tree_join_kernel<DT, 1><<<(unsigned)(((long long)a.U * R + 7) / 8), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
