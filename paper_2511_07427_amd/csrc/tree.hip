@@ -253,8 +253,8 @@ __device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, 
 
 enum Source { kList, kPacked8, kPacked4 };
 
-// How the L entries of a unit are shared: the same in the kernel that works and in the one that joins.
-__device__ __forceinline__ int splits_of(int L, int S, int chunk) { return min(S, max(1, L / chunk)); }
+// How the L entries of a unit are shared, `chunk` of them to a workgroup: the same in the kernel that works and in the one that joins.
+__device__ __forceinline__ int splits_of(int L, int S, int chunk) { return min(S, max(1, (L + chunk - 1) / chunk)); }
 
 // Writes the values of 16 or 32 codes (16 bytes) of one block to `to`.
 template <int DT, int BITS>
@@ -316,58 +316,102 @@ struct Stage<DT, kList, N> {
 
 template <int DT, int BITS, int N>
 struct StagePacked {
-  static constexpr int kBytes = kHeadDim * BITS / 8, kParts = kBytes / 16, kLoads = N * kParts / 64;
+  static constexpr int kBytes = kHeadDim * BITS / 8, kParts = kBytes / 16;         // 16-byte parts of a row
+  static constexpr bool kSplit = N * kParts < 64;                                 // the lower 32 lanes take the K rows, the upper ones the V rows
+  static constexpr int kLanes = kSplit ? 32 : 64, kLoads = N * kParts / kLanes;
+  static_assert(kLoads * kLanes == N * kParts, "every row once");
   uint4 k[kLoads], v[kLoads];
   uint32_t ks[kLoads], vs[kLoads];
   // rows first + r of the cache; beyond `left` rows the last one instead
   __device__ __forceinline__ void begin(const TreeArgs& a, size_t first, int left, int r0, int lane) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int r = min(r0 + (i * 64 + lane) / kParts, left - 1), part = lane % kParts;
-      const size_t row = first + r;
-      k[i] = *(const uint4*)((const char*)a.cache.k_codes + row * kBytes + part * 16);
-      v[i] = *(const uint4*)((const char*)a.cache.v_codes + row * kBytes + part * 16);
-      ks[i] = a.cache.k_scales[row * kRowScales + part * 4 / kParts];
-      vs[i] = a.cache.v_scales[row * kRowScales + part * 4 / kParts];
+      const int at = i * kLanes + lane % kLanes, r = min(r0 + at / kParts, left - 1), part = at % kParts;
+      const size_t row = first + r, code = row * kBytes + part * 16, scale = row * kRowScales + part * 4 / kParts;
+      const bool values = kSplit && lane >= 32;
+      k[i] = *(const uint4*)((const char*)(values ? a.cache.v_codes : a.cache.k_codes) + code);
+      ks[i] = (values ? a.cache.v_scales : a.cache.k_scales)[scale];
+      if constexpr (!kSplit) {
+        v[i] = *(const uint4*)((const char*)a.cache.v_codes + code);
+        vs[i] = a.cache.v_scales[scale];
+      }
     }
   }
   __device__ __forceinline__ void end(char* kt, char* vt, int left, int r0, int lane) {
+    using M = Mma<DT>;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int r = r0 + (i * 64 + lane) / kParts, part = lane % kParts;
+      const int at = i * kLanes + lane % kLanes, r = r0 + at / kParts, c = at % kParts * (M::kRow / kParts);
       const bool ok = r < left;
-      constexpr int wide = Mma<DT>::kRow / kParts;   // bytes of the values of a part
-      spread<DT, BITS>(kt + r * Mma<DT>::kRowK + part * wide, ok ? k[i] : uint4{0, 0, 0, 0}, ok ? scale_value(ks[i]) : 0.f);
-      spread<DT, BITS>(vt + r * Mma<DT>::kRowV + part * wide, ok ? v[i] : uint4{0, 0, 0, 0}, ok ? scale_value(vs[i]) : 0.f);
+      char *kto = kt + r * M::kRowK + c, *vto = vt + r * M::kRowV + c;
+      if constexpr (kSplit) kto = lane >= 32 ? vto : kto;
+      spread<DT, BITS>(kto, ok ? k[i] : uint4{0, 0, 0, 0}, ok ? scale_value(ks[i]) : 0.f);
+      if constexpr (!kSplit) spread<DT, BITS>(vto, ok ? v[i] : uint4{0, 0, 0, 0}, ok ? scale_value(vs[i]) : 0.f);
     }
   }
 };
 template <int DT, int N> struct Stage<DT, kPacked8, N> : StagePacked<DT, 8, N> {};
 template <int DT, int N> struct Stage<DT, kPacked4, N> : StagePacked<DT, 4, N> {};
 
-// grid: XCD-interleaved (unit, split) x row blocks.  Four wavefronts: WR of them take 32 rows each and share tiles of kSlots entries,
-// 4 / WR such groups take the split's tiles in turn.  The next tile is on its way in registers while one is consumed.
+// Rows of the drafted tokens, as Stage has those of the entries; `bad` gets a bit for every row with a value that is not finite, which goes in
+// as zero.
+template <int DT, int N>
+struct Drafts {
+  using M = Mma<DT>;
+  static constexpr int kPer = 64 * 16 / M::kRow, kLoads = N / kPer;
+  uint4 k[kLoads], v[kLoads];
+  __device__ __forceinline__ void begin(const TreeArgs& a, size_t first, int left, int r0, int lane) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const size_t at = (first + max(0, min(r0 + i * kPer + lane * 16 / M::kRow, left - 1))) * M::kRow + lane % (M::kRow / 16) * 16;
+      k[i] = *(const uint4*)((const char*)a.K1 + at);
+      v[i] = *(const uint4*)((const char*)a.V1 + at);
+    }
+  }
+  __device__ __forceinline__ void end(char* kt, char* vt, int left, int r0, int lane, unsigned long long& bad) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = r0 + i * kPer + lane * 16 / M::kRow, c = lane % (M::kRow / 16) * 16;
+      bool b = false;
+      uint4 vv = M::only_finite(v[i], b);
+      if (r >= left) { k[i] = uint4{0, 0, 0, 0}; vv = uint4{0, 0, 0, 0}; b = false; }
+      *(uint4*)(kt + r * M::kRowK + c) = k[i];
+      *(uint4*)(vt + r * M::kRowV + c) = vv;
+      const unsigned long long any = __ballot(b);
+#pragma unroll
+      for (int z = 0; z < kPer; ++z)
+        if ((any >> (z * (64 / kPer))) & (~0ull >> (64 - 64 / kPer))) bad |= 1ull << (r0 + i * kPer + z);
+    }
+  }
+};
+
+// A workgroup of W wavefronts, one per compute unit: WR of them take 32 rows each and share tiles of kSlots entries; W / WR such groups take
+// the tiles in turn.  Shared tiles have two places, of which one is filled while the other is read, with one barrier per tile.  A wavefront
+// that has its tiles alone (up to 32 rows: bound by memory) keeps 32 rows of K and V on their way in registers: 128 KB per compute unit.
 template <int DT, int SRC, int WR>
 struct Shape {
-  static constexpr int kGroups = 4 / WR, kSlots = WR == 4 ? 2 * kSub : kSub, kMine = kSlots / WR;   // rows of a tile that a wavefront loads
+  static constexpr int W = DT == DYNAKV_F32 ? 4 : 8, kThreads = 64 * W;
+  static constexpr int kGroups = W / WR, kSlots = WR >= 4 ? 2 * kSub : kSub, kMine = kSlots / WR, kPlaces = WR == 1 ? 1 : 2;   // kMine: rows of a tile that a wavefront loads
   static constexpr int kTileK = kSlots * Mma<DT>::kRowK, kTile = kTileK + kSlots * Mma<DT>::kRowV;     // bytes
   static constexpr int kOut = kHeadDim + 4;                                                         // floats of a row in the merge
-  static constexpr int kMerge = 4 * kSub * kOut * 4, kTiles = kGroups * kTile, kLds = kTiles > kMerge ? kTiles : kMerge;
+  static constexpr int kMerge = W * kSub * kOut * 4, kTiles = kGroups * kPlaces * kTile, kLds = kTiles > kMerge ? kTiles : kMerge;
+  static_assert(kLds <= 163840 - 256, "LDS of a compute unit");
 };
 
 template <int DT, int SRC, int WR>
-__global__ __launch_bounds__(256, DT == DYNAKV_F32 ? 1 : 2) void tree_kernel(TreeArgs a) {
+__global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(TreeArgs a) {
   using M = Mma<DT>;
   using Sh = Shape<DT, SRC, WR>;
-  constexpr int kOut = Sh::kOut, kSlots = Sh::kSlots, N = kSlots / kSub;
+  constexpr int kOut = Sh::kOut, kSlots = Sh::kSlots, N = kSlots / kSub, kGroups = Sh::kGroups, W = Sh::W;
   extern __shared__ __align__(16) char lds[];
+  __shared__ unsigned long long sbad[W];
   // workgroups with the same entries run on the same XCD, one after the other: they share its L2
   const int us = ((int)blockIdx.x >> 3) / a.RB * 8 + ((int)blockIdx.x & 7), rb = ((int)blockIdx.x >> 3) % a.RB;
   if (us >= a.U * a.S) return;
   const int u = us % a.U, s = us / a.U;              // units first: where a unit has fewer splits, all XCDs lack some
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int grp = wave / WR, wr = wave % WR;
-  const int R = a.T * a.G, row0 = (rb * WR + wr) * kSub, row = row0 + (lane & 31);
+  const int R = a.T * a.G, row = (rb * WR + wr) * kSub + (lane & 31);
   const bool live = row < R;
 
   int L, nlist = 0;
@@ -381,14 +425,28 @@ __global__ __launch_bounds__(256, DT == DYNAKV_F32 ? 1 : 2) void tree_kernel(Tre
   if (s >= ns) return;
   const int nt = (L + kSlots - 1) / kSlots, t0 = (int)((long long)nt * s / ns), t1 = (int)((long long)nt * (s + 1) / ns);
 
+  // the queries, the drafted tokens (the unit's last split; group g takes those from g kSlots on) and the first tile are requested together
   typename M::Q q;
   M::load_q(q, a.Q, (size_t)u * R + (live ? row : 0), h, live);
+  const int r0 = wr * Sh::kMine, j0 = grp * kSlots;
+  const bool drafts = a.K1 && s == ns - 1, mine = drafts && j0 < a.T;
+  unsigned long long word = 0;
+  Drafts<DT, Sh::kMine> draft;
+  auto node_bits = [&] {
+    const int node = (live ? row : 0) / a.G;
+    const unsigned long long w = a.tree ? a.tree[(size_t)u * a.T + node] : ~0ull >> (63 - node);
+    return a.T < 64 ? w & ((1ull << a.T) - 1) : w;
+  };
+  if (mine) {
+    draft.begin(a, (size_t)u * a.T + j0, a.T - j0, r0, lane);
+    word = node_bits() >> j0;
+  }
+
   Rows st;
   st.m = -__builtin_inff(); st.l = 0.f;
 #pragma unroll
   for (int d = 0; d < 4; ++d) st.o[d] = f16v{};
-  char* kt = lds + grp * Sh::kTile;
-  char* vt = kt + Sh::kTileK;
+  char* tiles = lds + grp * Sh::kPlaces * Sh::kTile;
 
   // a wavefront's own tile needs no barrier: its LDS operations keep their order, and so must the compiler
   auto sync = [] {
@@ -402,7 +460,6 @@ __global__ __launch_bounds__(256, DT == DYNAKV_F32 ? 1 : 2) void tree_kernel(Tre
   // at only there: a conditional load here, or a copy of what is on its way, would wait for every load before it.
   auto entry_index = [&](int t) { return t * (kSlots / 4) + (lane >> 2) % (kSlots / 4); };
   Stage<DT, SRC, Sh::kMine> stage;
-  const int r0 = wr * Sh::kMine;
   constexpr unsigned long long kAll = kSlots == 64 ? ~0ull : 0xFFFFFFFFull;
   int t = t0 + grp, entry = 0;
   unsigned long long seen = 0, seen_next = 0;        // slots of the tile that hold an entry
@@ -414,83 +471,83 @@ __global__ __launch_bounds__(256, DT == DYNAKV_F32 ? 1 : 2) void tree_kernel(Tre
       const int e = entry_index(tile) < nlist ? entry : -1;
       seen_next = __ballot(e >= 0 && (lane & 3) <= (e & 3)) & kAll;
       stage.begin(a, pages, e, r0, lane);
-      request_entry(tile + Sh::kGroups);
+      request_entry(tile + kGroups);
     } else {
       const int left = L - tile * kSlots;
       seen_next = left >= kSlots ? kAll : (1ull << left) - 1;
       stage.begin(a, first + (size_t)tile * kSlots, left, r0, lane);
     }
   };
+  auto end = [&](int tile, int place) {
+    char* kt = tiles + place * Sh::kTile;
+    if constexpr (SRC == kList) stage.end(kt, kt + Sh::kTileK, seen_next, seen_next == kAll, r0, lane);
+    else stage.end(kt, kt + Sh::kTileK, L - tile * kSlots, r0, lane);
+    seen = seen_next;
+  };
   if (t < t1) {
     request_entry(t);
     begin(t);
   }
-  __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0): the queries are there, and no iteration waits for them with the tile on its way
-  const int rounds = (t1 - t0 + Sh::kGroups - 1) / Sh::kGroups;      // of the whole workgroup: barriers are common
-  for (int i = 0; i < rounds; ++i, t += Sh::kGroups) {
-    const bool have = t < t1;
-    seen = seen_next;
-    if (have) {
-      if constexpr (SRC == kList) stage.end(kt, vt, seen, seen == kAll, r0, lane);
-      else stage.end(kt, vt, L - t * kSlots, r0, lane);
+
+  // the drafted tokens first, in the last place
+  constexpr int kLast = Sh::kPlaces - 1;
+  unsigned long long bad = 0;
+  if (drafts) {
+    char* kt = tiles + kLast * Sh::kTile;
+    if (mine) {
+      draft.end(kt, kt + Sh::kTileK, a.T - j0, r0, lane, bad);
+      if constexpr (WR > 1) sbad[wave] = bad;        // of the wavefront's share of the rows
     }
     sync();
-    if (t + Sh::kGroups < t1) begin(t + Sh::kGroups);
-    if (have) consume<DT, N>(st, kt, vt, q, seen == kAll, true, seen, a.sc, lane);
+    if (mine) {
+      if constexpr (WR > 1) {
+        bad = 0;
+        for (int w = 0; w < WR; ++w) bad |= sbad[grp * WR + w];
+      }
+      consume<DT, N>(st, kt, kt + Sh::kTileK, q, false, false, word, a.sc, lane);
+    }
+    asm volatile("" ::: "memory");
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0): the queries are there, and no iteration waits for them with the tile on its way
+
+  const int rounds = (t1 - t0 + kGroups - 1) / kGroups;      // of the whole workgroup: barriers are common
+  if (t < t1) {
+    end(t, 0);
+    if (t + kGroups < t1) begin(t + kGroups);
+  }
+  sync();
+  for (int i = 0; i < rounds; ++i, t += kGroups) {
+    char* kt = tiles + (kLast ? i & 1 : 0) * Sh::kTile;
+    const unsigned long long now = seen;
+    auto next = [&] {
+      if (t + kGroups < t1) {
+        end(t + kGroups, kLast ? (i + 1) & 1 : 0);
+        if (t + 2 * kGroups < t1) begin(t + 2 * kGroups);
+      }
+    };
+    if constexpr (kLast) next();                     // into the other place
+    if (kGroups == 1 || t < t1) consume<DT, N>(st, kt, kt + Sh::kTileK, q, now == kAll, true, now, a.sc, lane);
     sync();
+    if constexpr (!kLast) next();
+    if constexpr (!kLast) sync();
   }
 
-  // the drafted tokens: the unit's last split, tiles of 32, one for each of the first groups
-  const int j0 = grp * kSub;
-  if (s == ns - 1 && a.K1) {
-    constexpr int kPer = 64 * 16 / M::kRow, kTrees = Sh::kGroups >= 2 ? 1 : 2;
-    for (int w = 0; w < kTrees; ++w) {               // (a single group takes both)
-      const int j1 = j0 + w * kSub;
-      uint32_t bad = 0;
-      if (j1 < a.T) {
-#pragma unroll 2
-        for (int i = 0; i < kSub / kPer; ++i) {      // every wavefront of the group writes the same: they need not wait for each other
-          const int r = i * kPer + lane * 16 / M::kRow, c = lane % (M::kRow / 16) * 16;
-          uint4 kk = {0, 0, 0, 0}, vv = {0, 0, 0, 0};
-          bool b = false;
-          if (j1 + r < a.T) {
-            const size_t at = ((size_t)u * a.T + j1 + r) * M::kRow + c;
-            kk = *(const uint4*)((const char*)a.K1 + at);
-            vv = M::only_finite(*(const uint4*)((const char*)a.V1 + at), b);
-          }
-          *(uint4*)(kt + r * M::kRowK + c) = kk;
-          *(uint4*)(vt + r * M::kRowV + c) = vv;
-          const unsigned long long any = __ballot(b);
+  // Values of drafted tokens that are not finite went in as zeros, so that a row which does not see their token stays clean of them; the
+  // rows that see it get them here.
+  if (bad) {
+    const unsigned long long sees = node_bits() >> j0;
+    while (bad) {
+      const int j = __builtin_ctzll(bad);
+      bad &= bad - 1;
+      const size_t at = ((size_t)u * a.T + j0 + j) * kHeadDim;
 #pragma unroll
-          for (int z = 0; z < kPer; ++z)
-            if ((any >> (z * (64 / kPer))) & (~0ull >> (64 - 64 / kPer))) bad |= 1u << (i * kPer + z);
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float x = M::elem(a.V1, at + 32 * d + entry_of(i, 0) + 4 * h);
+          if (((sees >> j) & 1u) && !(fabsf(x) < __builtin_inff())) st.o[d][i] += x;
+          if (i % 8 == 7) hold_order();
         }
-      }
-      sync();
-      if (j1 < a.T) {
-        const int node = (live ? row : 0) / a.G;
-        unsigned long long bits = a.tree ? a.tree[(size_t)u * a.T + node] : ~0ull >> (63 - node);
-        if (a.T < 64) bits &= (1ull << a.T) - 1;
-        const uint32_t seen = (uint32_t)(bits >> j1);
-        consume<DT, 1>(st, kt, vt, q, false, false, seen, a.sc, lane);
-        // values that are not finite went in as zeros, so that a row which does not see their token stays clean of them;
-        // the rows that see it get them here
-        while (bad) {
-          const int j = __builtin_ctz(bad);
-          bad &= bad - 1;
-          const bool sees = (seen >> j) & 1u;
-          const size_t at = ((size_t)u * a.T + j1 + j) * kHeadDim;
-#pragma unroll
-          for (int d = 0; d < 4; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float x = M::elem(a.V1, at + 32 * d + entry_of(i, 0) + 4 * h);
-              if (sees && !(fabsf(x) < __builtin_inff())) st.o[d][i] += x;
-              if (i % 8 == 7) hold_order();
-            }
-        }
-      }
-      sync();
     }
   }
 
@@ -500,23 +557,23 @@ __global__ __launch_bounds__(256, DT == DYNAKV_F32 ? 1 : 2) void tree_kernel(Tre
   lds_barrier();
   float* mo = (float*)lds;
   {
-    float* mine = mo + ((size_t)wave * kSub + (lane & 31)) * kOut;
+    float* at = mo + ((size_t)wave * kSub + (lane & 31)) * kOut;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; i += 4) *(f4*)(mine + 32 * d + entry_of(i, h)) = f4{st.o[d][i], st.o[d][i + 1], st.o[d][i + 2], st.o[d][i + 3]};
-    if (h == 0) { mine[kHeadDim] = st.m; mine[kHeadDim + 1] = st.l; }
+      for (int i = 0; i < 16; i += 4) *(f4*)(at + 32 * d + entry_of(i, h)) = f4{st.o[d][i], st.o[d][i + 1], st.o[d][i + 2], st.o[d][i + 3]};
+    if (h == 0) { at[kHeadDim] = st.m; at[kHeadDim + 1] = st.l; }
   }
   lds_barrier();
-  for (int i = threadIdx.x; i < WR * kSub * (kHeadDim / 4); i += 256) {
+  for (int i = threadIdx.x; i < WR * kSub * (kHeadDim / 4); i += Sh::kThreads) {
     const int r = i >> 5, c = (i & 31) * 4, rr = rb * WR * kSub + r;      // row r of the workgroup: wavefront r / 32 of every group
     if (rr >= R) break;
-    float mw[Sh::kGroups], m = -__builtin_inff(), l = 0.f;
+    float mw[kGroups], m = -__builtin_inff(), l = 0.f;
 #pragma unroll
-    for (int w = 0; w < Sh::kGroups; ++w) { mw[w] = mo[(w * WR * kSub + r) * kOut + kHeadDim]; m = fmaxf(m, mw[w]); }
+    for (int w = 0; w < kGroups; ++w) { mw[w] = mo[(w * WR * kSub + r) * kOut + kHeadDim]; m = fmaxf(m, mw[w]); }
     f4 o = {0, 0, 0, 0};
 #pragma unroll
-    for (int w = 0; w < Sh::kGroups; ++w) {
+    for (int w = 0; w < kGroups; ++w) {
       if (mw[w] == -__builtin_inff()) continue;       // that wavefront saw nothing of this row
       const float f = mw[w] == m ? 1.f : __builtin_amdgcn_exp2f(mw[w] - m);
       const float* x = mo + (w * WR * kSub + r) * kOut;
@@ -586,15 +643,26 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   if (a.lse && c == 0) a.lse[i] = none ? m : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// Wavefronts of a workgroup that take rows of their own, up to four times 32 of the R rows of a unit.
-int row_waves(int dtype, int R) { return dtype == DYNAKV_F32 || R <= kSub ? 1 : R <= 2 * kSub ? 2 : 4; }
-// Workgroups that may share a unit's entries, so that about two workgroups per compute unit have work.
-int most_splits(int dtype, int U, int R) {
+// Wavefronts of a workgroup that take rows of their own, up to eight times 32 of the R rows of a unit.
+int row_waves(int dtype, int R) { return dtype == DYNAKV_F32 || R <= kSub ? 1 : R <= 2 * kSub ? 2 : R <= 4 * kSub ? 4 : 8; }
+
+// How many workgroups share the entries of a unit (at most `most` of them): the fewest of those whose time is least by this model.  256
+// workgroups run at once; one takes 6 us to begin and end and 30 ns for an entry; joining takes 4 us and moves 1056 bytes per
+// row and workgroup at 5 TB/s.
+int plan_splits(int dtype, int U, int R, long long most) {
   const int rows = row_waves(dtype, R) * kSub;
-  const long long wgs = (long long)U * ((R + rows - 1) / rows);
-  const long long s = (512 + wgs - 1) / wgs;
-  return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+  const long long n = (long long)U * ((R + rows - 1) / rows);
+  int best = 1;
+  double least = 0.0;
+  for (int s = 1; s <= 64; ++s) {
+    const double rounds = (double)((n * s + 255) / 256);
+    const double t = rounds * (6e3 + 30.0 * (double)most / s) + (s > 1 ? 4e3 + (double)U * s * R * 1056.0 / 5e3 : 0.0);
+    if (s == 1 || t < 0.97 * least) { best = s; least = t; }
+  }
+  return best;
 }
+// No call takes more than it would for very many entries.
+int most_splits(int dtype, int U, int R) { return plan_splits(dtype, U, R, 1ll << 31); }
 
 template <int DT, int SRC, int WR>
 hipError_t launch_shape(TreeArgs& a, hipStream_t st) {
@@ -602,7 +670,7 @@ hipError_t launch_shape(TreeArgs& a, hipStream_t st) {
   const int R = a.T * a.G;
   a.RB = (R + WR * kSub - 1) / (WR * kSub);
   const long long us = ((long long)a.U * a.S + 7) / 8 * 8;
-  tree_kernel<DT, SRC, WR><<<(unsigned)(us * a.RB), 256, Sh::kLds, st>>>(a);
+  tree_kernel<DT, SRC, WR><<<(unsigned)(us * a.RB), Sh::kThreads, Sh::kLds, st>>>(a);
   return hipGetLastError();
 }
 
@@ -612,17 +680,18 @@ hipError_t launch_source(TreeArgs& a, hipStream_t st) {
     return launch_shape<DT, SRC, 1>(a, st);
   } else {
     const int wr = row_waves(DT, a.T * a.G);
-    return wr == 1 ? launch_shape<DT, SRC, 1>(a, st) : wr == 2 ? launch_shape<DT, SRC, 2>(a, st) : launch_shape<DT, SRC, 4>(a, st);
+    return wr == 1   ? launch_shape<DT, SRC, 1>(a, st)
+           : wr == 2 ? launch_shape<DT, SRC, 2>(a, st)
+           : wr == 4 ? launch_shape<DT, SRC, 4>(a, st)
+                     : launch_shape<DT, SRC, 8>(a, st);
   }
 }
 
 template <int DT>
 hipError_t launch(TreeArgs a, hipStream_t st) {
   const int R = a.T * a.G;
-  a.S = most_splits(DT, a.U, R);
-  // a partial result costs a row 2 * 528 bytes of traffic: a workgroup's share of the entries is several times that
-  a.chunk = R < 64 ? 256 : 4 * R;
-  a.S = min(a.S, max(1, a.most / a.chunk));         // (more would have nothing to do)
+  a.S = min(plan_splits(DT, a.U, R, a.most), most_splits(DT, a.U, R));
+  a.chunk = max(64, (a.most + a.S - 1) / a.S);
   const hipError_t e = a.pages ? launch_source<DT, kList>(a, st) : a.cache.bits == 8 ? launch_source<DT, kPacked8>(a, st) : launch_source<DT, kPacked4>(a, st);
   if (e != hipSuccess) return e;
   if (a.S > 8) tree_join_kernel<DT, 8><<<(unsigned)((long long)a.U * R), 256, 0, st>>>(a);
