@@ -51,7 +51,7 @@ struct Mma {
     else
       return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
   }
-  // Scores of N tiles of 32 entries each, kSub rows apart.  The operands of a step are requested two steps before it.
+  // Adds the scores of N tiles of 32 entries each, kSub rows apart.  The operands of a step are requested two steps before it.
   template <int N>
   static __device__ __forceinline__ void qk(f16v (&c)[N], const char* k, const Q& q, int lane) {
     const char* at = k + (lane & 31) * kRowK + (lane >> 5) * 16;
@@ -60,8 +60,6 @@ struct Mma {
 #pragma unroll
       for (int n = 0; n < N; ++n) f[s][n] = *(const uint4*)(at + n * kSub * kRowK + s * 32);
     };
-#pragma unroll
-    for (int n = 0; n < N; ++n) c[n] = f16v{};
     request(0);
     request(1);
 #pragma unroll
@@ -127,8 +125,6 @@ struct Mma<DYNAKV_F32> {
   static __device__ __forceinline__ void qk(f16v (&c)[N], const char* k, const Q& q, int lane) {
     const char* at = k + (lane & 31) * kRowK + (lane >> 5) * 16;
 #pragma unroll
-    for (int n = 0; n < N; ++n) c[n] = f16v{};
-#pragma unroll
     for (int s = 0; s < 16; ++s)
 #pragma unroll
       for (int n = 0; n < N; ++n) {
@@ -167,36 +163,41 @@ struct Rows {
   f16v o[4];
 };
 
-// N tiles of 32 entries; full: every row sees all of them, else bit t of `seen` is set if the lane's row sees entry t (0 where the
-// slot holds none).  Slots that hold nothing have zeros in V.
+// What the scores of 32 slots begin with: 0, or -inf where a slot holds nothing.  (Conditions per slot on the finished scores, the same
+// for every row, took as many instructions as the exponentials.)
+__device__ __forceinline__ f16v begin_scores(const float* bias, int lane) {
+  f16v c;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const f4 x = *(const f4*)(bias + 8 * g + 4 * (lane >> 5));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[4 * g + i] = x[i];
+  }
+  return c;
+}
+// N tiles of 32 entries.  ALIKE: every row sees the same slots, those with a bias of 0; else bit t of `seen` is set if the lane's row sees
+// entry t.  Slots that hold nothing have zeros in K and V.
 // The accumulators are rescaled only when a maximum has grown by more than 2^8 since they were last: until then weights grow up to 2^8,
 // which no type minds, and 64 products per tile and row are saved in all but a few tiles.
 constexpr float kLazy = 8.f;
-template <int DT, int N>
-__device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, const typename Mma<DT>::Q& q, bool full, bool alike, unsigned long long seen, float sc,
-                                        int lane) {
+template <int DT, int N, bool ALIKE>
+__device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, const float* bias, const typename Mma<DT>::Q& q, unsigned long long seen, float sc, int lane) {
   using M = Mma<DT>;
   f16v s[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    if constexpr (ALIKE) s[n] = begin_scores(bias + n * kSub, lane);
+    else s[n] = f16v{};
+  }
   M::template qk<N>(s, k, q, lane);
   [[maybe_unused]] typename M::VFrag f[2];
   if constexpr (DT != DYNAKV_F32) M::load_v(f[0], v, 0, lane);       // arrives while the maxima are taken
-  if (!full) {
-    if (alike) {                                     // the same slots for every row: the conditions are scalars
+  if constexpr (!ALIKE) {
 #pragma unroll
-      for (int n = 0; n < N; ++n)
+    for (int n = 0; n < N; ++n) {
+      const uint32_t mine = (uint32_t)(seen >> (32 * n)) >> (4 * (lane >> 5));
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int e = 32 * n + entry_of(i, 0);
-          const unsigned long long lo = (seen >> e) & 1 ? 0xFFFFFFFFull : 0, hi = (seen >> (e + 4)) & 1 ? 0xFFFFFFFF00000000ull : 0;
-          s[n][i] = __builtin_amdgcn_inverse_ballot_w64(lo | hi) ? s[n][i] : -__builtin_inff();
-        }
-    } else {
-#pragma unroll
-      for (int n = 0; n < N; ++n) {
-        const uint32_t mine = (uint32_t)(seen >> (32 * n)) >> (4 * (lane >> 5));
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[n][i] = (mine >> entry_of(i, 0)) & 1u ? s[n][i] : -__builtin_inff();
-      }
+      for (int i = 0; i < 16; ++i) s[n][i] = (mine >> entry_of(i, 0)) & 1u ? s[n][i] : -__builtin_inff();
     }
   }
   float mx = -__builtin_inff();
@@ -392,7 +393,7 @@ template <int DT, int SRC, int WR>
 struct Shape {
   static constexpr int W = DT == DYNAKV_F32 ? 4 : 8, kThreads = 64 * W;
   static constexpr int kGroups = W / WR, kSlots = WR >= 4 ? 2 * kSub : kSub, kMine = kSlots / WR, kPlaces = WR == 1 ? 1 : 2;   // kMine: rows of a tile that a wavefront loads
-  static constexpr int kTileK = kSlots * Mma<DT>::kRowK, kTile = kTileK + kSlots * Mma<DT>::kRowV;     // bytes
+  static constexpr int kTileK = kSlots * Mma<DT>::kRowK, kTileV = kSlots * Mma<DT>::kRowV, kTile = kTileK + kTileV + kSlots * 4;   // bytes: K, V, bias
   static constexpr int kOut = kHeadDim + 4;                                                         // floats of a row in the merge
   static constexpr int kMerge = W * kSub * kOut * 4, kTiles = kGroups * kPlaces * kTile, kLds = kTiles > kMerge ? kTiles : kMerge;
   static_assert(kLds <= 163840 - 256, "LDS of a compute unit");
@@ -462,7 +463,7 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
   Stage<DT, SRC, Sh::kMine> stage;
   constexpr unsigned long long kAll = kSlots == 64 ? ~0ull : 0xFFFFFFFFull;
   int t = t0 + grp, entry = 0;
-  unsigned long long seen = 0, seen_next = 0;        // slots of the tile that hold an entry
+  unsigned long long seen_next = 0;                  // slots of the tile on its way that hold an entry
   auto request_entry = [&](int tile) {
     if constexpr (SRC == kList) entry = plist[min(entry_index(tile), nlist - 1)];
   };
@@ -480,9 +481,9 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
   };
   auto end = [&](int tile, int place) {
     char* kt = tiles + place * Sh::kTile;
+    if (lane < Sh::kMine) ((float*)(kt + Sh::kTileK + Sh::kTileV))[r0 + lane] = (seen_next >> (r0 + lane)) & 1 ? 0.f : -__builtin_inff();
     if constexpr (SRC == kList) stage.end(kt, kt + Sh::kTileK, seen_next, seen_next == kAll, r0, lane);
     else stage.end(kt, kt + Sh::kTileK, L - tile * kSlots, r0, lane);
-    seen = seen_next;
   };
   if (t < t1) {
     request_entry(t);
@@ -504,7 +505,7 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
         bad = 0;
         for (int w = 0; w < WR; ++w) bad |= sbad[grp * WR + w];
       }
-      consume<DT, N>(st, kt, kt + Sh::kTileK, q, false, false, word, a.sc, lane);
+      consume<DT, N, false>(st, kt, kt + Sh::kTileK, nullptr, q, word, a.sc, lane);
     }
     asm volatile("" ::: "memory");
   }
@@ -518,7 +519,6 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
   sync();
   for (int i = 0; i < rounds; ++i, t += kGroups) {
     char* kt = tiles + (kLast ? i & 1 : 0) * Sh::kTile;
-    const unsigned long long now = seen;
     auto next = [&] {
       if (t + kGroups < t1) {
         end(t + kGroups, kLast ? (i + 1) & 1 : 0);
@@ -526,7 +526,7 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
       }
     };
     if constexpr (kLast) next();                     // into the other place
-    if (kGroups == 1 || t < t1) consume<DT, N>(st, kt, kt + Sh::kTileK, q, now == kAll, true, now, a.sc, lane);
+    if (kGroups == 1 || t < t1) consume<DT, N, true>(st, kt, kt + Sh::kTileK, (const float*)(kt + Sh::kTileK + Sh::kTileV), q, 0, a.sc, lane);
     sync();
     if constexpr (!kLast) next();
     if constexpr (!kLast) sync();
