@@ -257,28 +257,58 @@ enum Source { kList, kPacked8, kPacked4 };
 // How the L entries of a unit are shared, `chunk` of them to a workgroup: the same in the kernel that works and in the one that joins.
 __device__ __forceinline__ int splits_of(int L, int S, int chunk) { return min(S, max(1, (L + chunk - 1) / chunk)); }
 
+// Two codes of a block (elements 2 i and 2 i + 1 of the eight or four in w) as float16 values.  A biased code c + 2^(BITS - 1) in the
+// low bits of the float16 1024 is the value 1024 + c + 2^(BITS - 1), in bits 4..7 it is 1024 + 16 (c + 8): a byte permutation, and the
+// arithmetic is packed and exact.  (Two instructions per value where conversion through float32 takes four and a half.)
+template <int BITS>
+__device__ __forceinline__ uint32_t pair_f16(uint32_t biased, int i, h2 scale) {
+  if constexpr (BITS == 8) {
+    const uint32_t x = __builtin_amdgcn_perm(0x64646464u, biased, i ? 0x04030402u : 0x04010400u);
+    return __builtin_bit_cast(uint32_t, (__builtin_bit_cast(h2, x) - (h2){(_Float16)1152.f, (_Float16)1152.f}) * scale);
+  } else {
+    const uint32_t x = __builtin_amdgcn_perm(0x64646464u, biased, 0x04000400u + 0x00010001u * i) & 0xFFF0FF0Fu;
+    const h2 c = __builtin_elementwise_fma(__builtin_bit_cast(h2, x), (h2){(_Float16)1.f, (_Float16)0.0625f}, (h2){(_Float16)-1032.f, (_Float16)-72.f});
+    return __builtin_bit_cast(uint32_t, c * scale);
+  }
+}
+
 // Writes the values of 16 or 32 codes (16 bytes) of one block to `to`.
 template <int DT, int BITS>
 __device__ __forceinline__ void spread(char* to, uint4 w4, float scale) {
   constexpr int kVals = 128 / BITS, per = 16 / Mma<DT>::kES;   // values per chunk of the tile
   const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+  if constexpr (DT == DYNAKV_F16) {
+    const _Float16 s = (_Float16)scale;
+    constexpr int kPairs = 16 / BITS;                // per word of codes
 #pragma unroll
-  for (int c = 0; c < kVals / per; ++c) {
-    uint32_t o[4];
-    float x[per];
+    for (int c = 0; c < kVals / per; ++c) {
+      uint32_t o[4];
 #pragma unroll
-    for (int k = 0; k < per; ++k) {
-      const int i = c * per + k, bit = (i * BITS) & 31;
-      x[k] = (float)((int)(w[(i * BITS) >> 5] << (32 - BITS - bit)) >> (32 - BITS)) * scale;
+      for (int k = 0; k < 4; ++k) o[k] = pair_f16<BITS>(w[(4 * c + k) / kPairs] ^ (BITS == 8 ? 0x80808080u : 0x88888888u), (4 * c + k) % kPairs, (h2){s, s});
+      *(uint4*)(to + 16 * c) = uint4{o[0], o[1], o[2], o[3]};
     }
-    if constexpr (DT == DYNAKV_F32) {
+  } else {
+    // a signed byte is converted in one instruction; a 4-bit code in the upper half of a byte counts 16 times
+    const float s = BITS == 8 ? scale : scale * 0.0625f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] = __float_as_uint(x[k]);
-    } else {
+    for (int c = 0; c < kVals / per; ++c) {
+      uint32_t o[4];
+      float x[per];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] = Mma<DT>::round2(x[2 * k], x[2 * k + 1]);   // exact
+      for (int k = 0; k < per; ++k) {
+        const int i = c * per + k;
+        const uint32_t from = BITS == 8 ? w[i / 4] : (i & 1 ? w[i / 8] : w[i / 8] << 4) & 0xF0F0F0F0u;
+        x[k] = (float)(int8_t)(from >> (8 * (BITS == 8 ? i % 4 : i % 8 / 2))) * s;
+      }
+      if constexpr (DT == DYNAKV_F32) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = __float_as_uint(x[k]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = __builtin_amdgcn_perm(__float_as_uint(x[2 * k + 1]), __float_as_uint(x[2 * k]), 0x07060302u);   // exact: the lower halves are zero
+      }
+      *(uint4*)(to + 16 * c) = uint4{o[0], o[1], o[2], o[3]};
     }
-    *(uint4*)(to + 16 * c) = uint4{o[0], o[1], o[2], o[3]};
   }
 }
 
