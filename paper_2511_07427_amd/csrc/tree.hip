@@ -40,10 +40,10 @@ template <int DT>
 struct Mma {
   static constexpr int kES = 2, kRow = kHeadDim * 2, kRowK = kRow + 16, kRowV = kRow + 32;   // in memory, in LDS
   struct Q { uint4 b[8]; };
-  static __device__ __forceinline__ void load_q(Q& q, const void* base, size_t row, int h, bool ok) {
+  static __device__ __forceinline__ void load_q(Q& q, const void* base, size_t row, int h) {
     const char* p = (const char*)base + row * kRow + 16 * h;
 #pragma unroll
-    for (int s = 0; s < 8; ++s) q.b[s] = ok ? *(const uint4*)(p + 32 * s) : uint4{0, 0, 0, 0};
+    for (int s = 0; s < 8; ++s) q.b[s] = *(const uint4*)(p + 32 * s);
   }
   static __device__ __forceinline__ f16v mma(uint4 a, uint4 b, f16v c) {
     if constexpr (DT == DYNAKV_BF16)
@@ -98,6 +98,11 @@ struct Mma {
   static __device__ __forceinline__ void store4(void* out, size_t i, f4 x) {
     *(uint2*)((uint16_t*)out + i) = uint2{round2(x[0], x[1]), round2(x[2], x[3])};
   }
+  // Bits 15 and 31: whether the elements of w are no finite numbers (their exponent is all ones, and carries).
+  static __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+    constexpr uint32_t ex = DT == DYNAKV_BF16 ? 0x7F807F80u : 0x7C007C00u, low = DT == DYNAKV_BF16 ? 0x00800080u : 0x04000400u;
+    return ((w & ex) + low) & 0x80008000u;
+  }
   // a chunk with zeros for the elements that are no finite numbers; bad: there was one
   static __device__ __forceinline__ uint4 only_finite(uint4 a, bool& bad) {
     constexpr uint32_t ex = DT == DYNAKV_BF16 ? 0x7F80u : 0x7C00u;
@@ -116,10 +121,10 @@ struct Mma<DYNAKV_F32> {
   struct VFrag {};
   static constexpr int kES = 4, kRow = kHeadDim * 4, kRowK = kRow + 16, kRowV = kRow + 32;
   struct Q { f4 b[16]; };
-  static __device__ __forceinline__ void load_q(Q& q, const void* base, size_t row, int h, bool ok) {
+  static __device__ __forceinline__ void load_q(Q& q, const void* base, size_t row, int h) {
     const char* p = (const char*)base + row * kRow + 16 * h;
 #pragma unroll
-    for (int s = 0; s < 16; ++s) q.b[s] = ok ? *(const f4*)(p + 32 * s) : f4{0, 0, 0, 0};
+    for (int s = 0; s < 16; ++s) q.b[s] = *(const f4*)(p + 32 * s);
   }
   template <int N>
   static __device__ __forceinline__ void qk(f16v (&c)[N], const char* k, const Q& q, int lane) {
@@ -148,6 +153,7 @@ struct Mma<DYNAKV_F32> {
   }
   static __device__ __forceinline__ float elem(const void* base, size_t i) { return ((const float*)base)[i]; }
   static __device__ __forceinline__ void store4(void* out, size_t i, f4 x) { *(f4*)((float*)out + i) = x; }
+  static __device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7F800000u) + 0x00800000u) & 0x80000000u; }
   static __device__ __forceinline__ uint4 only_finite(uint4 a, bool& bad) {
     uint32_t* w = (uint32_t*)&a;
 #pragma unroll
@@ -175,24 +181,22 @@ __device__ __forceinline__ f16v begin_scores(const float* bias, int lane) {
   }
   return c;
 }
-// N tiles of 32 entries.  ALIKE: every row sees the same slots, those with a bias of 0; else bit t of `seen` is set if the lane's row sees
-// entry t.  Slots that hold nothing have zeros in K and V.
+// N tiles of 32 entries.  Of a tile of the cache every row sees the same slots, those with a bias of 0; of drafted tokens (their bias is 0) those
+// whose bit is set in `seen`.  Slots that hold nothing have zeros in K and V.
 // The accumulators are rescaled only when a maximum has grown by more than 2^8 since they were last: until then weights grow up to 2^8,
 // which no type minds, and 64 products per tile and row are saved in all but a few tiles.
 constexpr float kLazy = 8.f;
-template <int DT, int N, bool ALIKE>
-__device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, const float* bias, const typename Mma<DT>::Q& q, unsigned long long seen, float sc, int lane) {
+template <int DT, int N>
+__device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, const float* bias, const typename Mma<DT>::Q& q, bool drafts, unsigned long long seen, float sc,
+                                        int lane) {
   using M = Mma<DT>;
   f16v s[N];
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    if constexpr (ALIKE) s[n] = begin_scores(bias + n * kSub, lane);
-    else s[n] = f16v{};
-  }
+  for (int n = 0; n < N; ++n) s[n] = begin_scores(bias + n * kSub, lane);
   M::template qk<N>(s, k, q, lane);
   [[maybe_unused]] typename M::VFrag f[2];
   if constexpr (DT != DYNAKV_F32) M::load_v(f[0], v, 0, lane);       // arrives while the maxima are taken
-  if constexpr (!ALIKE) {
+  if (drafts) {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const uint32_t mine = (uint32_t)(seen >> (32 * n)) >> (4 * (lane >> 5));
@@ -400,18 +404,27 @@ struct Drafts {
     }
   }
   __device__ __forceinline__ void end(char* kt, char* vt, int left, int r0, int lane, unsigned long long& bad) {
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) any |= M::not_finite(v[i].x) | M::not_finite(v[i].y) | M::not_finite(v[i].z) | M::not_finite(v[i].w);
+    if (__any(any != 0)) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int r = r0 + i * kPer + lane * 16 / M::kRow;
+        bool b = false;
+        v[i] = M::only_finite(v[i], b);
+        const unsigned long long rows = __ballot(b && r < left);
+#pragma unroll
+        for (int z = 0; z < kPer; ++z)
+          if ((rows >> (z * (64 / kPer))) & (~0ull >> (64 - 64 / kPer))) bad |= 1ull << (r0 + i * kPer + z);
+      }
+    }
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int r = r0 + i * kPer + lane * 16 / M::kRow, c = lane % (M::kRow / 16) * 16;
-      bool b = false;
-      uint4 vv = M::only_finite(v[i], b);
-      if (r >= left) { k[i] = uint4{0, 0, 0, 0}; vv = uint4{0, 0, 0, 0}; b = false; }
+      if (r >= left) { k[i] = uint4{0, 0, 0, 0}; v[i] = uint4{0, 0, 0, 0}; }
       *(uint4*)(kt + r * M::kRowK + c) = k[i];
-      *(uint4*)(vt + r * M::kRowV + c) = vv;
-      const unsigned long long any = __ballot(b);
-#pragma unroll
-      for (int z = 0; z < kPer; ++z)
-        if ((any >> (z * (64 / kPer))) & (~0ull >> (64 - 64 / kPer))) bad |= 1ull << (r0 + i * kPer + z);
+      *(uint4*)(vt + r * M::kRowV + c) = v[i];
     }
   }
 };
@@ -443,7 +456,6 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int grp = wave / WR, wr = wave % WR;
   const int R = a.T * a.G, row = (rb * WR + wr) * kSub + (lane & 31);
-  const bool live = row < R;
 
   int L, nlist = 0;
   if constexpr (SRC == kList) {
@@ -458,13 +470,13 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
 
   // the queries, the drafted tokens (the unit's last split; group g takes those from g kSlots on) and the first tile are requested together
   typename M::Q q;
-  M::load_q(q, a.Q, (size_t)u * R + (live ? row : 0), h, live);
+  M::load_q(q, a.Q, (size_t)u * R + min(row, R - 1), h);      // (rows beyond the last: its queries; not written)
   const int r0 = wr * Sh::kMine, j0 = grp * kSlots;
   const bool drafts = a.K1 && s == ns - 1, mine = drafts && j0 < a.T;
   unsigned long long word = 0;
   Drafts<DT, Sh::kMine> draft;
   auto node_bits = [&] {
-    const int node = (live ? row : 0) / a.G;
+    const int node = min(row, R - 1) / a.G;
     const unsigned long long w = a.tree ? a.tree[(size_t)u * a.T + node] : ~0ull >> (63 - node);
     return a.T < 64 ? w & ((1ull << a.T) - 1) : w;
   };
@@ -515,39 +527,25 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
     if constexpr (SRC == kList) stage.end(kt, kt + Sh::kTileK, seen_next, seen_next == kAll, r0, lane);
     else stage.end(kt, kt + Sh::kTileK, L - tile * kSlots, r0, lane);
   };
+  constexpr int kLast = Sh::kPlaces - 1;
+  unsigned long long bad = 0;
   if (t < t1) {
     request_entry(t);
     begin(t);
   }
-
-  // the drafted tokens first, in the last place
-  constexpr int kLast = Sh::kPlaces - 1;
-  unsigned long long bad = 0;
-  if (drafts) {
-    char* kt = tiles + kLast * Sh::kTile;
-    if (mine) {
-      draft.end(kt, kt + Sh::kTileK, a.T - j0, r0, lane, bad);
-      if constexpr (WR > 1) sbad[wave] = bad;        // of the wavefront's share of the rows
-    }
-    sync();
-    if (mine) {
-      if constexpr (WR > 1) {
-        bad = 0;
-        for (int w = 0; w < WR; ++w) bad |= sbad[grp * WR + w];
-      }
-      consume<DT, N, false>(st, kt, kt + Sh::kTileK, nullptr, q, word, a.sc, lane);
-    }
-    asm volatile("" ::: "memory");
+  if (mine) {                                        // the drafted tokens, to the last place
+    char* to = tiles + kLast * Sh::kTile;
+    draft.end(to, to + Sh::kTileK, a.T - j0, r0, lane, bad);
+    if (lane < Sh::kMine) ((float*)(to + Sh::kTileK + Sh::kTileV))[r0 + lane] = 0.f;
+    if constexpr (WR > 1) sbad[wave] = bad;          // of the wavefront's share of the rows
   }
-  __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0): the queries are there, and no iteration waits for them with the tile on its way
-
-  const int rounds = (t1 - t0 + kGroups - 1) / kGroups;      // of the whole workgroup: barriers are common
-  if (t < t1) {
-    end(t, 0);
-    if (t + kGroups < t1) begin(t + kGroups);
-  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0): the queries are there, and no round waits for them with a tile on its way
   sync();
-  for (int i = 0; i < rounds; ++i, t += kGroups) {
+  // Round i reads the tiles of place i & 1 (where there are two), writes the next ones to the other and requests those after them; round -1 reads
+  // the drafted tokens.  One copy of the code for all of them: a workgroup's first rounds run from a cold instruction cache.
+  const int rounds = (t1 - t0 + kGroups - 1) / kGroups;      // of the whole workgroup: barriers are common
+  t -= kGroups;
+  for (int i = -1; i < rounds; ++i, t += kGroups) {
     char* kt = tiles + (kLast ? i & 1 : 0) * Sh::kTile;
     auto next = [&] {
       if (t + kGroups < t1) {
@@ -556,10 +554,18 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
       }
     };
     if constexpr (kLast) next();                     // into the other place
-    if (kGroups == 1 || t < t1) consume<DT, N, true>(st, kt, kt + Sh::kTileK, (const float*)(kt + Sh::kTileK + Sh::kTileV), q, 0, a.sc, lane);
+    if (i < 0 ? mine : kGroups == 1 || t < t1)
+      consume<DT, N>(st, kt, kt + Sh::kTileK, (const float*)(kt + Sh::kTileK + Sh::kTileV), q, i < 0, word, a.sc, lane);
     sync();
-    if constexpr (!kLast) next();
-    if constexpr (!kLast) sync();
+    if constexpr (!kLast) {
+      next();
+      sync();
+    }
+  }
+  if constexpr (WR > 1) {
+    bad = 0;
+    if (mine)
+      for (int w = 0; w < WR; ++w) bad |= sbad[grp * WR + w];
   }
 
   // Values of drafted tokens that are not finite went in as zeros, so that a row which does not see their token stays clean of them; the
