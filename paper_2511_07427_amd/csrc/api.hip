@@ -448,7 +448,7 @@ static dynakv_status_t tree_args(TreeArgs* a, int U, int T, int G, int dtype, fl
   a->U = U; a->T = T; a->G = G; a->dtype = dtype;
   a->sc = scale * 1.4426950408889634f;
   a->Q = Q; a->K1 = K1; a->V1 = V1; a->tree = (const unsigned long long*)tree;
-  a->out = out; a->lse = lse; a->part = (float*)scratch;
+  a->out = out; a->lse = lse; a->scratch = scratch;
   return DYNAKV_OK;
 }
 

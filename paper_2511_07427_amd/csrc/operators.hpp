@@ -36,7 +36,7 @@ struct TreeArgs {
   const unsigned long long* tree;                   // null: a chain
   void* out;
   float* lse;
-  float* part;                                      // [U][S][T * G][kPartRow]
+  void* scratch;
   int most;                                         // no unit has more entries than this, as far as the host knows
   // the entries: the gather list of an index ...
   const char* pages;                                // null: a packed cache
@@ -46,10 +46,12 @@ struct TreeArgs {
   // ... or rows of a packed cache
   dynakv_packed_t cache;
   const int* lengths;
-  // launch shape (plan_tree)
-  int S;                                            // most workgroups that share the entries of a unit
-  int RB;                                           // blocks of rows
-  int chunk;                                        // entries that a workgroup takes at least, where several share a unit
+  // set by launch_tree
+  int RB;                                           // blocks of rows of a unit
+  int pieces;                                       // most workgroups for each; U: every unit whole
+  int least;                                        // entries for which another workgroup is worth it
+  int* where;                                       // [U][2] first piece and pieces of a unit
+  float* part;                                      // [pieces][T * G][kPartRow]
 };
 constexpr int kPartRow = kHeadDim + 4;              // accumulators, maximum, denominator, padding to 16 bytes
 size_t tree_scratch_bytes(int U, int T, int G);

@@ -28,6 +28,8 @@ typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kSub = 32;                             // entries of one matrix tile, rows of a wavefront
+constexpr int kWorkgroups = 256;                     // that run at once: one per compute unit
+constexpr int kPlanUnits = 512;                      // of more units none is shared
 
 // Keeps the loads of what follows from being moved up in front of what came before, where their results fill the registers.
 __device__ __forceinline__ void hold_order() { __builtin_amdgcn_sched_barrier(0); }
@@ -258,8 +260,72 @@ __device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, 
 
 enum Source { kList, kPacked8, kPacked4 };
 
-// How the L entries of a unit are shared, `chunk` of them to a workgroup: the same in the kernel that works and in the one that joins.
-__device__ __forceinline__ int splits_of(int L, int S, int chunk) { return min(S, max(1, (L + chunk - 1) / chunk)); }
+template <int SRC>
+__device__ __forceinline__ int slots_of(const TreeArgs& a, int u) {
+  if constexpr (SRC == kList) return 4 * a.n_list[u];
+  else return a.lengths ? min(max(a.lengths[u], 0), a.cache.capacity) : a.cache.capacity;
+}
+
+// A unit's entries are shared by ceil(entries / chunk) workgroups, `chunk` the smallest (to a sixteenth) with which all units together make no
+// more than a.pieces: that many run in whole rounds of the chip, however much the units differ.  All workgroups find the same chunk,
+// each for itself in one wavefront.  Piece q of all is piece `first` + s of unit u's `count`.
+struct Piece { int u, s, count, first, slots; };
+template <int SRC>
+__device__ __forceinline__ Piece piece_of(const TreeArgs& a, int q, int lane) {
+  if (a.pieces == a.U || a.U > kPlanUnits) return Piece{q, 0, 1, q, q < a.U ? slots_of<SRC>(a, q) : 0};   // whole units
+  constexpr int kPer = kPlanUnits / 64;
+  int len[kPer], most = 0;
+  float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int u = lane + 64 * k;
+    len[k] = u < a.U ? slots_of<SRC>(a, u) : -1;
+    most = max(most, len[k]);
+    sum += (float)max(len[k], 0);
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+  most = wave_max(most);
+  // of a unit (the thousandth: a unit of no more than `chunk` entries is one piece, whatever the product's rounding)
+  auto count_of = [](int n, float inv) { return max(1, (int)ceilf((float)n * inv - 1e-3f)); };
+  auto fits = [&](int chunk) {
+    const float inv = 1.f / (float)chunk;
+    int c = 0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k)
+      if (64 * k < a.U) c += len[k] >= 0 ? count_of(len[k], inv) : 0;
+    return wave_sum(c) <= a.pieces;
+  };
+  // pieces >= sum / chunk, pieces <= sum / chunk + units
+  int lo = max(a.least, (int)fminf(sum / (float)a.pieces, 1e9f)), hi = max(lo, most);
+  if (!fits(lo)) {
+    hi = max(lo + 1, min(hi, (int)fminf(sum / (float)(a.pieces - a.U), 1e9f) + 2));
+    if (!fits(hi)) hi = max(hi, most);               // (one piece each)
+    while (hi - lo > lo / 16 + 1) {
+      const int mid = lo + (hi - lo) / 2;
+      if (fits(mid)) hi = mid;
+      else lo = mid;
+    }
+  } else {
+    hi = lo;
+  }
+  const float inv = 1.f / (float)hi;
+  int base = 0;
+  Piece p = {-1, 0, 1, 0, 0};
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    if (64 * k >= a.U) break;
+    const int c = len[k] >= 0 ? count_of(len[k], inv) : 0, end = base + wave_incl_scan(c);
+    const unsigned long long here = __ballot(end - c <= q && q < end);
+    if (here) {
+      const int l = __builtin_ctzll(here);
+      p = Piece{l + 64 * k, q - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(c, l)), __builtin_amdgcn_readlane(c, l),
+                __builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(c, l), __builtin_amdgcn_readlane(len[k], l)};
+    }
+    base = __builtin_amdgcn_readlane(end, 63);
+  }
+  return p;                                          // u < 0: there are fewer pieces
+}
 
 // Two codes of a block (elements 2 i and 2 i + 1 of the eight or four in w) as float16 values.  A biased code c + 2^(BITS - 1) in the
 // low bits of the float16 1024 is the value 1024 + c + 2^(BITS - 1), in bits 4..7 it is 1024 + 16 (c + 8): a byte permutation, and the
@@ -450,23 +516,21 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
   extern __shared__ __align__(16) char lds[];
   __shared__ unsigned long long sbad[W];
   // workgroups with the same entries run on the same XCD, one after the other: they share its L2
-  const int us = ((int)blockIdx.x >> 3) / a.RB * 8 + ((int)blockIdx.x & 7), rb = ((int)blockIdx.x >> 3) % a.RB;
-  if (us >= a.U * a.S) return;
-  const int u = us % a.U, s = us / a.U;              // units first: where a unit has fewer splits, all XCDs lack some
+  const int piece = ((int)blockIdx.x >> 3) / a.RB * 8 + ((int)blockIdx.x & 7), rb = ((int)blockIdx.x >> 3) % a.RB;
+  if (piece >= a.pieces) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int grp = wave / WR, wr = wave % WR;
   const int R = a.T * a.G, row = (rb * WR + wr) * kSub + (lane & 31);
-
-  int L, nlist = 0;
-  if constexpr (SRC == kList) {
-    nlist = a.n_list[u];
-    L = 4 * nlist;
-  } else {
-    L = a.lengths ? min(max(a.lengths[u], 0), a.cache.capacity) : a.cache.capacity;
-  }
-  const int ns = splits_of(L, a.S, a.chunk);
-  if (s >= ns) return;
+  const Piece pc = piece_of<SRC>(a, piece, lane);
+  if (pc.u < 0) return;
+  const int u = __builtin_amdgcn_readfirstlane(pc.u), ns = __builtin_amdgcn_readfirstlane(pc.count), s = __builtin_amdgcn_readfirstlane(pc.s);
+  const int L = __builtin_amdgcn_readfirstlane(pc.slots);
+  [[maybe_unused]] const int nlist = L / 4;
   const int nt = (L + kSlots - 1) / kSlots, t0 = (int)((long long)nt * s / ns), t1 = (int)((long long)nt * (s + 1) / ns);
+  if (a.pieces != a.U && rb == 0 && s == 0 && threadIdx.x == 0) {      // for the kernel that joins
+    a.where[2 * u] = __builtin_amdgcn_readfirstlane(pc.first);
+    a.where[2 * u + 1] = ns;
+  }
 
   // the queries, the drafted tokens (the unit's last split; group g takes those from g kSlots on) and the first tile are requested together
   typename M::Q q;
@@ -622,15 +686,15 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
       M::store4(a.out, to * kHeadDim + c, none ? f4{0, 0, 0, 0} : o / l);
       if (a.lse && c == 0) a.lse[to] = none ? m : (m + __builtin_amdgcn_logf(l)) * kLn2;
     } else {
-      float* p = a.part + (((size_t)u * a.S + s) * R + rr) * kPartRow;
+      float* p = a.part + ((size_t)piece * R + rr) * kPartRow;
       *(f4*)(p + c) = o;
       if (c == 0) { p[kHeadDim] = m; p[kHeadDim + 1] = l; }
     }
   }
 }
 
-// Joins the splits of the units that have several.  32 lanes take up to eight partial results of a row at once; of more, P = 8 such groups
-// share a row (64 partial results one after the other, each a trip to memory, took 52 us).
+// Joins the pieces of the units that have several, in their order.  P groups of 32 lanes share a row and take eight pieces at once (64 of
+// them one after the other, each a trip to memory, took 52 us).
 template <int DT, int P>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   __shared__ __align__(16) float sm[8][kPartRow];
@@ -638,30 +702,37 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   const size_t i = (size_t)blockIdx.x * (8 / P) + grp / P;
   if (P < 8 && i >= (size_t)a.U * R) return;
   const int u = (int)(i / R), r = (int)(i % R);
-  const int L = a.pages ? 4 * a.n_list[u] : a.lengths ? min(max(a.lengths[u], 0), a.cache.capacity) : a.cache.capacity;
-  const int ns = splits_of(L, a.S, a.chunk);
+  const int first = a.where[2 * u], ns = a.where[2 * u + 1];
   if (ns == 1) return;                               // (P = 8: the whole workgroup)
-  const float* p = a.part + ((size_t)u * a.S * R + r) * kPartRow;
+  const float* p = a.part + ((size_t)first * R + r) * kPartRow;
   float ms[8], ls[8], m = -__builtin_inff(), l = 0.f;
   f4 os[8], o = {0, 0, 0, 0};
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const int s = grp % P + P * k;
-    const float* x = p + (size_t)min(s, ns - 1) * R * kPartRow;
-    ms[k] = s < ns ? x[kHeadDim] : -__builtin_inff();
-    ls[k] = x[kHeadDim + 1];
-    os[k] = *(const f4*)(x + c);
-  }
   auto add = [&](float mk, float lk, const f4& ok) {
     if (mk == -__builtin_inff()) return;             // saw nothing of this row, whatever its sums hold
     const float f = mk == m ? 1.f : __builtin_amdgcn_exp2f(mk - m);
     l += f * lk;
     o += f * ok;
   };
+  for (int s0 = grp % P; s0 < ns; s0 += 8 * P) {
 #pragma unroll
-  for (int k = 0; k < 8; ++k) m = fmaxf(m, ms[k]);
+    for (int k = 0; k < 8; ++k) {
+      const int s = s0 + P * k;
+      const float* x = p + (size_t)min(s, ns - 1) * R * kPartRow;
+      ms[k] = s < ns ? x[kHeadDim] : -__builtin_inff();
+      ls[k] = x[kHeadDim + 1];
+      os[k] = *(const f4*)(x + c);
+    }
+    float top = m;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) add(ms[k], ls[k], os[k]);
+    for (int k = 0; k < 8; ++k) top = fmaxf(top, ms[k]);
+    if (top == -__builtin_inff()) continue;
+    const float f = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+    m = top;
+    l *= f;
+    o *= f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) add(ms[k], ls[k], os[k]);
+  }
   if constexpr (P == 8) {
     *(f4*)&sm[grp][c] = o;
     if (c == 0) { sm[grp][kHeadDim] = m; sm[grp][kHeadDim + 1] = l; }
@@ -682,31 +753,43 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
 // Wavefronts of a workgroup that take rows of their own, up to eight times 32 of the R rows of a unit.
 int row_waves(int dtype, int R) { return dtype == DYNAKV_F32 || R <= kSub ? 1 : R <= 2 * kSub ? 2 : R <= 4 * kSub ? 4 : 8; }
 
-// How many workgroups share the entries of a unit (at most `most` of them): the fewest of those whose time is least by this model.  256
-// workgroups run at once; one takes 6 us to begin and end and 30 ns for an entry; joining takes 4 us and moves 1056 bytes per
-// row and workgroup at 5 TB/s.
-int plan_splits(int dtype, int U, int R, long long most) {
-  const int rows = row_waves(dtype, R) * kSub;
-  const long long n = (long long)U * ((R + rows - 1) / rows);
-  int best = 1;
-  double least = 0.0;
-  for (int s = 1; s <= 64; ++s) {
-    const double rounds = (double)((n * s + 255) / 256);
-    const double t = rounds * (6e3 + 30.0 * (double)most / s) + (s > 1 ? 4e3 + (double)U * s * R * 1056.0 / 5e3 : 0.0);
-    if (s == 1 || t < 0.97 * least) { best = s; least = t; }
-  }
-  return best;
+// Workgroups that a call gets for each block of rows (`pieces`), and the fewest entries for which another one is worth it (`least`), from a
+// model in ns, measured on 1 to 256 units: 256 workgroups run at once; one takes 9 us to begin and end, and per entry the larger of its
+// bytes (at its share of 5 TB/s, at most 64 per ns) and the work of its rows; the kernel that joins takes 6 us.  Units of one length would be
+// cut into s pieces each; a multiple of 256 workgroups that has room for those is what units of any lengths share.
+struct Plan { int pieces, least; };
+constexpr int kMostRounds = 4;                       // bounds the scratch
+int row_blocks(int dtype, int R) { return (R + row_waves(dtype, R) * kSub - 1) / (row_waves(dtype, R) * kSub); }
+bool may_share(int dtype, int U, int R) { return U <= kPlanUnits && (long long)U * row_blocks(dtype, R) <= 2 * kWorkgroups; }
+int pieces_for(int dtype, int U, int R, int s) {     // a unit of s pieces: 0: more rounds than there may be
+  const int rb = row_blocks(dtype, R), rounds = (U * rb * s + kWorkgroups - 1) / kWorkgroups;
+  return rounds > kMostRounds ? 0 : max(U, rounds * kWorkgroups / rb);
 }
-// No call takes more than it would for very many entries.
-int most_splits(int dtype, int U, int R) { return plan_splits(dtype, U, R, 1ll << 31); }
+Plan plan(int dtype, int bytes, int U, int R, long long most, bool ragged) {
+  if (!may_share(dtype, U, R)) return Plan{U, 1};
+  const int n = U * row_blocks(dtype, R);
+  const double work = dtype == DYNAKV_F32 ? 34.0 : 4.0 * row_waves(dtype, R);      // (the float32 matrix instructions)
+  auto entry = [&](int workgroups) {
+    const double share = 5120.0 / (workgroups < kWorkgroups ? workgroups : kWorkgroups), b = bytes / (share < 64.0 ? share : 64.0);
+    return b > work ? b : work;
+  };
+  if (entry(n) * (double)most < 8e3) return Plan{U, 1};
+  int best = 0;
+  double time = 0.0;
+  for (int s = 1; s <= 64 && pieces_for(dtype, U, R, s); ++s) {
+    const double t = (double)((n * s + kWorkgroups - 1) / kWorkgroups) * (9e3 + entry(n * s) * (double)most / s) + (s > 1 ? 6e3 : 0.0);
+    if (s == 1 || t < 0.97 * time) { best = s; time = t; }
+  }
+  if (best == 0 || (best == 1 && !ragged)) return Plan{U, 1};
+  return Plan{pieces_for(dtype, U, R, best), (int)(4e3 / entry(kWorkgroups)) + 1};
+}
 
 template <int DT, int SRC, int WR>
 hipError_t launch_shape(TreeArgs& a, hipStream_t st) {
   using Sh = Shape<DT, SRC, WR>;
   const int R = a.T * a.G;
   a.RB = (R + WR * kSub - 1) / (WR * kSub);
-  const long long us = ((long long)a.U * a.S + 7) / 8 * 8;
-  tree_kernel<DT, SRC, WR><<<(unsigned)(us * a.RB), Sh::kThreads, Sh::kLds, st>>>(a);
+  tree_kernel<DT, SRC, WR><<<(unsigned)((a.pieces + 7ll) / 8 * 8 * a.RB), Sh::kThreads, Sh::kLds, st>>>(a);
   return hipGetLastError();
 }
 
@@ -725,25 +808,36 @@ hipError_t launch_source(TreeArgs& a, hipStream_t st) {
 
 template <int DT>
 hipError_t launch(TreeArgs a, hipStream_t st) {
-  const int R = a.T * a.G;
-  a.S = min(plan_splits(DT, a.U, R, a.most), most_splits(DT, a.U, R));
-  a.chunk = max(64, (a.most + a.S - 1) / a.S);
+  const int R = a.T * a.G, bytes = a.pages ? 2 * Mma<DT>::kRow : 2 * (kHeadDim * a.cache.bits / 8 + kRowScales);
+  const Plan p = plan(DT, bytes, a.U, R, a.most, !a.pages && a.lengths);
+  a.pieces = p.pieces;
+  a.least = p.least;
   const hipError_t e = a.pages ? launch_source<DT, kList>(a, st) : a.cache.bits == 8 ? launch_source<DT, kPacked8>(a, st) : launch_source<DT, kPacked4>(a, st);
-  if (e != hipSuccess) return e;
-  if (a.S > 8) tree_join_kernel<DT, 8><<<(unsigned)((long long)a.U * R), 256, 0, st>>>(a);
-  else if (a.S > 1) tree_join_kernel<DT, 1><<<(unsigned)(((long long)a.U * R + 7) / 8), 256, 0, st>>>(a);
+  if (e != hipSuccess || a.pieces == a.U) return e;
+  if (a.pieces > 8 * a.U) tree_join_kernel<DT, 8><<<(unsigned)((long long)a.U * R), 256, 0, st>>>(a);
+  else tree_join_kernel<DT, 1><<<(unsigned)(((long long)a.U * R + 7) / 8), 256, 0, st>>>(a);
   return hipGetLastError();
+}
+
+// Scratch: where the pieces of each unit are, then a partial result of every row for each piece.  The most that any plan has.
+size_t where_bytes(int U) { return ((size_t)U * 8 + 255) & ~(size_t)255; }
+size_t part_bytes(int dtype, int U, int R) {
+  int most = 0;
+  for (int s = 1; may_share(dtype, U, R) && s <= 64; ++s) most = max(most, pieces_for(dtype, U, R, s));
+  return (size_t)most * R * kPartRow * sizeof(float);
 }
 
 }  // namespace
 
 size_t tree_scratch_bytes(int U, int T, int G) {
-  const size_t R = (size_t)T * G;
-  const int s16 = most_splits(DYNAKV_F16, U, (int)R), s32 = most_splits(DYNAKV_F32, U, (int)R), S = s16 > s32 ? s16 : s32;
-  return 256 + (S > 1 ? (size_t)U * S * R * kPartRow * sizeof(float) : 0);
+  const size_t a = part_bytes(DYNAKV_F16, U, T * G), b = part_bytes(DYNAKV_F32, U, T * G);
+  return where_bytes(U) + (a > b ? a : b);
 }
 
-hipError_t launch_tree(const TreeArgs& a, hipStream_t st) {
+hipError_t launch_tree(const TreeArgs& in, hipStream_t st) {
+  TreeArgs a = in;
+  a.where = (int*)a.scratch;
+  a.part = (float*)((char*)a.scratch + where_bytes(a.U));
   if (a.dtype == DYNAKV_F32) return launch<DYNAKV_F32>(a, st);
   if (a.dtype == DYNAKV_F16) return launch<DYNAKV_F16>(a, st);
   return launch<DYNAKV_BF16>(a, st);
