@@ -14,32 +14,6 @@ namespace {
 
 typedef uint16_t us4 __attribute__((ext_vector_type(4)));
 
-// Four consecutive elements (8-byte aligned for 16-bit types, 16 for float32).
-template <int DT>
-__device__ __forceinline__ void load4(const void* base, size_t i, float (&x)[4]) {
-  if constexpr (DT == DYNAKV_F32) {
-    const f4 a = *(const f4*)((const float*)base + i);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = a[e];
-  } else {
-    const us4 a = *(const us4*)((const uint16_t*)base + i);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = DT == DYNAKV_F16 ? f16_to_float(a[e]) : bf16_to_float(a[e]);
-  }
-}
-template <int DT>
-__device__ __forceinline__ void store4(void* base, size_t i, const float (&x)[4]) {
-  if constexpr (DT == DYNAKV_F32) {
-    *(f4*)((float*)base + i) = f4{x[0], x[1], x[2], x[3]};
-  } else {
-    us4 a;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      a[e] = DT == DYNAKV_F16 ? __builtin_bit_cast(uint16_t, (_Float16)x[e]) : __builtin_bit_cast(uint16_t, (__bf16)x[e]);
-    *(us4*)((uint16_t*)base + i) = a;
-  }
-}
-
 // Sum over a row of 16 lanes, the same bits in every lane.
 __device__ __forceinline__ float row16_sum(float x) {
   auto add = [&](int y) { x += __int_as_float(y); };
@@ -50,62 +24,162 @@ __device__ __forceinline__ float row16_sum(float x) {
   return x;
 }
 
-// grid (tokens, chunks of heads); 16 rows at a time, `per` of them by each row of 16 lanes.
+// How a lane's eight elements of a row lie: kNear: 8 l .. 8 l + 7 (neighbouring pairs, or no rotation); kHalf: the whole head is rotated in pairs
+// 64 apart: the lane loads those eight too, and lanes l and l + 8 exchange four of them; kApart: other pairs rotary_dim / 2 apart: two runs of four,
+// loaded as they are needed (8-byte loads move 7 % less than 16-byte loads and the exchange).
+enum Order { kNear, kHalf, kApart };
+
+// Four elements as they lie in memory.
 template <int DT>
+struct Four;
+template <>
+struct Four<DYNAKV_F32> {
+  typedef f4 T;
+  static __device__ __forceinline__ void get(T a, float (&x)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = a[e];
+  }
+  static __device__ __forceinline__ T put(const float (&x)[4]) { return f4{x[0], x[1], x[2], x[3]}; }
+};
+template <int DT>
+struct Four16 {
+  typedef us4 T;
+  static __device__ __forceinline__ void get(T a, float (&x)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = DT == DYNAKV_F16 ? f16_to_float(a[e]) : bf16_to_float(a[e]);
+  }
+  static __device__ __forceinline__ T put(const float (&x)[4]) {
+    us4 a;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      a[e] = DT == DYNAKV_F16 ? __builtin_bit_cast(uint16_t, (_Float16)x[e]) : __builtin_bit_cast(uint16_t, (__bf16)x[e]);
+    return a;
+  }
+};
+template <> struct Four<DYNAKV_F16> : Four16<DYNAKV_F16> {};
+template <> struct Four<DYNAKV_BF16> : Four16<DYNAKV_BF16> {};
+
+// The four elements of the lane eight lanes away in the row of 16.
+template <class T>
+__device__ __forceinline__ T across(T x) {
+  constexpr int n = sizeof(T) / 4;
+  int w[n];
+  __builtin_memcpy(w, &x, sizeof(T));
+#pragma unroll
+  for (int i = 0; i < n; ++i) w[i] = __builtin_amdgcn_update_dpp(0, w[i], 0x128, 0xF, 0xF, false);   // row_ror:8
+  __builtin_memcpy(&x, w, sizeof(T));
+  return x;
+}
+// kHalf: (elements 8 l .., 8 l + 4 ..) of lanes l and l + 8 <-> a lane's four first and four second members of pairs.  Its own inverse.
+template <class T>
+__device__ __forceinline__ void exchange(T& x, T& y, bool upper) {
+  const T got = across(upper ? x : y);
+  if (upper) x = got;
+  else y = got;
+}
+
+// Workgroup (token, chunk of 16 a.per heads); each row of 16 lanes takes `per` heads, kBatch of them on their way at once.  All rows go the
+// same way through the code, values too (their result is dropped): with branches and 64-bit address arithmetic per kind of row the kernel
+// had as much to issue as to move (191 us for 16384 tokens of 80 rows).
+template <int DT, int ORDER>
 __global__ __launch_bounds__(256) void norm_rope_kernel(HeadsArgs a) {
+  using F = Four<DT>;
+  typedef typename F::T T;
+  constexpr int kBatch = 4;
+  constexpr size_t kRowBytes = kHeadDim / 4 * sizeof(T);
   const dynakv_heads_t& c = a.c;
   const int b = blockIdx.x / c.n_tokens, t = blockIdx.x % c.n_tokens;
   const int pos = a.positions[blockIdx.x];
   if (pos < 0) return;
   const int lane = threadIdx.x & 15, row = threadIdx.x >> 4;
   const int H = c.n_kv_heads, G = c.group_size, nq = H * G, heads = nq + 2 * H, rot = c.rotary_dim;
+  const bool upper = lane >= 8;
   const bool turns = 8 * lane < rot;
-  // the lane's two runs of four elements
-  const bool apart = !c.interleaved && rot > 0;      // pairs half the rotated part apart
-  const int i0 = apart ? (turns ? 4 * lane : 8 * lane) : 8 * lane, i1 = apart && turns ? rot / 2 + 4 * lane : i0 + 4;
-  float cs[4], sn[4];
+  // the lane's two runs of four elements in memory
+  const int i0 = ORDER == kApart && turns ? 4 * lane : 8 * lane, i1 = ORDER == kApart && turns ? rot / 2 + 4 * lane : i0 + 4;
+  const int pair = ORDER == kHalf ? 8 * (lane & 7) + (upper ? 4 : 0) : 4 * lane;      // the first of its four pairs
+
+  // the token's rows: in, out, and what separates heads out there (in rows)
+  const int64_t es = sizeof(T) / 4;
+  const char* in[3] = {(const char*)a.q + ((int64_t)b * c.q_seq_stride + (int64_t)t * c.q_token_stride) * es,
+                       (const char*)a.k + ((int64_t)b * c.k_seq_stride + (int64_t)t * c.k_token_stride) * es,
+                       (const char*)a.v + ((int64_t)b * c.v_seq_stride + (int64_t)t * c.v_token_stride) * es};
+  const size_t first = (size_t)b * H * c.n_tokens + t;
+  char* out[3] = {(char*)a.Q + first * G * kRowBytes, (char*)a.K + first * kRowBytes, (char*)a.V + first * kRowBytes};
+  const bool there[3] = {a.q != nullptr, a.k != nullptr, a.v != nullptr};
+  const float per_group = 1.f / (float)G;
+  const int past_group = G * (c.n_tokens - 1);
+  struct Head { bool isq, isv, ok; const char* from; char* to; };
+  auto head = [&](int h, int h1) {
+    Head x;
+    x.isq = h < nq;
+    x.isv = h >= nq + H;
+    const int hh = x.isq ? h : x.isv ? h - nq - H : h - nq;
+    x.ok = h < h1 && (x.isq ? there[0] : x.isv ? there[2] : there[1]);
+    x.from = (x.isq ? in[0] : x.isv ? in[2] : in[1]) + (size_t)((unsigned)hh * (unsigned)kRowBytes);
+    const int kv = (int)(((float)hh + 0.5f) * per_group);        // hh / G (exact: hh < 2^19)
+    x.to = (x.isq ? out[0] : x.isv ? out[2] : out[1]) + (size_t)(unsigned)(x.isq ? hh + kv * past_group : hh * c.n_tokens) * kRowBytes;
+    return x;
+  };
+
+  const int h0 = blockIdx.y * 16 * a.per + row, h1 = min(heads, (int)(blockIdx.y + 1) * 16 * a.per);
+  float cs[4], sn[4], w[2][8];
+  for (int hb = h0; hb < h1; hb += 16 * kBatch) {
+    T lo[kBatch], hi[kBatch];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    cs[e] = 1.f; sn[e] = 0.f;
-    if (turns) {
-      double r = (double)pos * (double)a.inv_freq[4 * lane + e] * 0.15915494309189533577;
-      r -= rint(r);
-      sincospif(2.f * (float)r, &sn[e], &cs[e]);
+    for (int k = 0; k < kBatch; ++k) {
+      const Head x = head(hb + 16 * k, h1);
+      if (!x.ok) continue;
+      lo[k] = ((const T*)x.from)[i0 / 4];
+      hi[k] = ((const T*)x.from)[i1 / 4];
     }
-  }
-  const int h0 = blockIdx.y * 16 * a.per + row;
-  for (int k = 0; k < a.per; ++k) {
-    const int h = h0 + 16 * k;
-    if (h >= heads) break;
-    const int what = h < nq ? 0 : h < nq + H ? 1 : 2, hh = what == 0 ? h : what == 1 ? h - nq : h - nq - H;
-    const void* src = what == 0 ? a.q : what == 1 ? a.k : a.v;
-    if (!src) continue;
-    const int64_t ss = what == 0 ? c.q_seq_stride : what == 1 ? c.k_seq_stride : c.v_seq_stride;
-    const int64_t st = what == 0 ? c.q_token_stride : what == 1 ? c.k_token_stride : c.v_token_stride;
-    const size_t from = (size_t)((int64_t)b * ss + (int64_t)t * st) + (size_t)hh * kHeadDim;
-    float x[4], y[4];
-    load4<DT>(src, from + i0, x);
-    load4<DT>(src, from + i1, y);
-    size_t to;
-    if (what == 0) to = (((size_t)(b * H + hh / G) * c.n_tokens + t) * G + hh % G) * kHeadDim;
-    else to = ((size_t)(b * H + hh) * c.n_tokens + t) * kHeadDim;
-    if (what < 2) {
-      const void* w = what == 0 ? a.wq : a.wk;
-      if (w) {
-        float s = 0.f;
+    if (hb == h0) {                                  // while the first rows are on their way
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s += x[e] * x[e];
+      for (int z = 0; z < 2; ++z) {
+        const void* from = z ? a.wk : a.wq;
+        float f[4] = {1.f, 1.f, 1.f, 1.f}, g[4] = {1.f, 1.f, 1.f, 1.f};
+        if (from) {
+          T x = ((const T*)from)[i0 / 4], y = ((const T*)from)[i1 / 4];
+          if (ORDER == kHalf) exchange(x, y, upper);
+          F::get(x, f);
+          F::get(y, g);
+        }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s += y[e] * y[e];
-        const float r = rsqrtf(row16_sum(s) * (1.f / kHeadDim) + c.eps);
-        float wx[4], wy[4];
-        load4<DT>(w, i0, wx);
-        load4<DT>(w, i1, wy);
+        for (int e = 0; e < 4; ++e) { w[z][e] = f[e]; w[z][4 + e] = g[e]; }
+      }
+      float freq[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { x[e] = x[e] * r * wx[e]; y[e] = y[e] * r * wy[e]; }
+      for (int e = 0; e < 4; ++e) freq[e] = turns ? a.inv_freq[pair + e] : 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        double r = (double)pos * (double)freq[e] * 0.15915494309189533577;       // turns
+        r -= rint(r);
+        sincospif(2.f * (float)r, &sn[e], &cs[e]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const Head d = head(hb + 16 * k, h1);
+      if (!d.ok) continue;
+      T u = lo[k], v = hi[k];
+      if (ORDER == kHalf) exchange(u, v, upper);
+      float x[4], y[4];
+      F::get(u, x);
+      F::get(v, y);
+      float s = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s += x[e] * x[e];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s += y[e] * y[e];
+      const bool normed = d.isq ? a.wq != nullptr : a.wk != nullptr;
+      const float r = normed ? rsqrtf(row16_sum(s) * (1.f / kHeadDim) + c.eps) : 1.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = x[e] * r * (d.isq ? w[0][e] : w[1][e]);
+        y[e] = y[e] * r * (d.isq ? w[0][4 + e] : w[1][4 + e]);
       }
       if (turns) {
-        if (apart) {
+        if (ORDER != kNear) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float p = x[e], q = y[e];
@@ -115,19 +189,30 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(HeadsArgs a) {
         } else {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float p = x[2 * e], q = x[2 * e + 1], r = y[2 * e], s = y[2 * e + 1];
+            const float p = x[2 * e], q = x[2 * e + 1], f = y[2 * e], g = y[2 * e + 1];
             x[2 * e] = p * cs[e] - q * sn[e];
             x[2 * e + 1] = q * cs[e] + p * sn[e];
-            y[2 * e] = r * cs[2 + e] - s * sn[2 + e];
-            y[2 * e + 1] = s * cs[2 + e] + r * sn[2 + e];
+            y[2 * e] = f * cs[2 + e] - g * sn[2 + e];
+            y[2 * e + 1] = g * cs[2 + e] + f * sn[2 + e];
           }
         }
       }
+      u = F::put(x);
+      v = F::put(y);
+      if (ORDER == kHalf) exchange(u, v, upper);
+      ((T*)d.to)[i0 / 4] = d.isv ? lo[k] : u;
+      ((T*)d.to)[i1 / 4] = d.isv ? hi[k] : v;
     }
-    void* dst = what == 0 ? a.Q : what == 1 ? a.K : a.V;
-    store4<DT>(dst, to + i0, x);
-    store4<DT>(dst, to + i1, y);
   }
+}
+
+template <int DT>
+hipError_t launch(const HeadsArgs& a, dim3 grid, hipStream_t st) {
+  const int order = a.c.interleaved || a.c.rotary_dim == 0 ? kNear : a.c.rotary_dim == kHeadDim ? kHalf : kApart;
+  if (order == kNear) norm_rope_kernel<DT, kNear><<<grid, 256, 0, st>>>(a);
+  else if (order == kHalf) norm_rope_kernel<DT, kHalf><<<grid, 256, 0, st>>>(a);
+  else norm_rope_kernel<DT, kApart><<<grid, 256, 0, st>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -135,13 +220,11 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(HeadsArgs a) {
 hipError_t launch_norm_rope(const HeadsArgs& in, hipStream_t st) {
   HeadsArgs a = in;
   const int heads = a.c.n_kv_heads * (a.c.group_size + 2);
-  const size_t tokens = (size_t)a.c.n_seqs * a.c.n_tokens;
-  a.per = 1;
+  const long long tokens = (long long)a.c.n_seqs * a.c.n_tokens;
+  // Few tokens: a workgroup for every 16 rows, so that the chip has work; many: the angles of a token are taken once for up to 128 rows.
+  a.per = tokens * ((heads + 15) / 16) <= 2048 ? 1 : 8;
   const dim3 grid((unsigned)tokens, (heads + 16 * a.per - 1) / (16 * a.per));
-  if (a.c.dtype == DYNAKV_F32) norm_rope_kernel<DYNAKV_F32><<<grid, 256, 0, st>>>(a);
-  else if (a.c.dtype == DYNAKV_F16) norm_rope_kernel<DYNAKV_F16><<<grid, 256, 0, st>>>(a);
-  else norm_rope_kernel<DYNAKV_BF16><<<grid, 256, 0, st>>>(a);
-  return hipGetLastError();
+  return a.c.dtype == DYNAKV_F32 ? launch<DYNAKV_F32>(a, grid, st) : a.c.dtype == DYNAKV_F16 ? launch<DYNAKV_F16>(a, grid, st) : launch<DYNAKV_BF16>(a, grid, st);
 }
 
 }  // namespace dynakv
