@@ -153,35 +153,36 @@ def _dev(t: torch.Tensor, dtype, shape=None) -> int:
     return t.data_ptr()
 
 
-class _on:
-    """Makes the device of the tensors of a call current while it enqueues; value: that device's current stream."""
-
-    def __init__(self, device):
-        self.device = device
-
-    def __enter__(self):
-        self.before = torch.cuda.current_device()
-        if self.device.index != self.before:
-            torch.cuda.set_device(self.device.index)
-        return torch.cuda.current_stream(self.device.index).cuda_stream
-
-    def __exit__(self, *_):
-        if self.device.index != self.before:
-            torch.cuda.set_device(self.before)
+def _raw_stream(index: int) -> int:
+    return torch.cuda.current_stream(index).cuda_stream
 
 
-def _on_device(t, device, dtype, shape) -> int:
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)      # the same without making a Stream object (1 us)
+
+
+def _enqueue(index: int, name: str, call, *args):
+    """call(*args, stream) with the tensors' device current, on that device's current stream."""
+    if index == torch.cuda.current_device():
+        rc = call(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            rc = call(*args, _raw_stream(index))
+    if rc:
+        _check(rc, name)
+
+
+def _on_device(t, index: int, dtype, shape) -> int:
     """Address of an operand of the operators beside the index; ValueError where it does not fit."""
-    if t.device != device or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
-        raise ValueError("expected a contiguous %s tensor %s on %s, got %s %s on %s%s" % (
-            dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device, "" if t.is_contiguous() else ", not contiguous"))
+    if t.get_device() != index or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError("expected a contiguous %s tensor %s on GPU %d, got %s %s on %s%s" % (
+            dtype, tuple(shape), index, t.dtype, tuple(t.shape), t.device, "" if t.is_contiguous() else ", not contiguous"))
     return t.data_ptr()
 
 
-def _gpu(t: torch.Tensor) -> torch.device:
+def _gpu(t: torch.Tensor) -> int:
     if not t.is_cuda:
         raise ValueError("expected a tensor on a GPU, got one on %s" % t.device)
-    return t.device
+    return t.get_device()
 
 
 # ---- operators beside the index ---------------------------------------------------------------------
@@ -196,39 +197,47 @@ def dynakv_norm_rope(q, k, v, positions, q_out, k_out, v_out, q_weight=None, k_w
     are); any of them may be None together with its output.  positions int32 [B, T], negative: padding, left as it is.
     q_out [B * H, T, G, 128], k_out and v_out [B * H, T, 128]; q_weight, k_weight [128] or None: no norm; inv_freq float32
     [rotary_dim / 2] or None: no rotation."""
-    given = [(x, o) for x, o in ((q, q_out), (k, k_out), (v, v_out)) if x is not None]
-    if not given or any((x is None) != (o is None) for x, o in ((q, q_out), (k, k_out), (v, v_out))):
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (v is None) != (v_out is None):
         raise ValueError("queries, keys and values each come with their output")
-    first = given[0][0]
-    device, dtype = _gpu(first), first.dtype
+    given = q if q is not None else k if k is not None else v
+    if given is None:
+        raise ValueError("no rows are given")
+    index, dtype = _gpu(given), given.dtype
     if dtype not in _CODES:
         raise ValueError("rows of %s are not supported" % dtype)
+    if positions.dim() != 2 or given.dim() != 4:
+        raise ValueError("positions are [sequences, tokens], rows [sequences, tokens, heads, 128]")
     B, T = positions.shape
     kv = k if k is not None else v
     H = kv.shape[2] if kv is not None else q_out.shape[0] // max(1, B)
-    if H < 1 or (q is not None and (q.shape[2] % H or q.shape[2] == 0)):
-        raise ValueError("%d query heads do not go with %d KV heads" % (q.shape[2], H))
-    G = q.shape[2] // H if q is not None else 1
-    c = _Heads(_CODES[dtype], B, T, H, G, 128, 0 if inv_freq is None else 2 * inv_freq.numel(), int(bool(interleaved)), eps)
-    for name, x, heads in (("q", q, H * G), ("k", k, H), ("v", v, H)):
+    heads = H if q is None else q.shape[2]
+    if H < 1 or heads < 1 or heads % H:
+        raise ValueError("%d query heads do not go with %d KV heads" % (heads, H))
+    G = heads // H
+
+    def rows(x, n, name):                  # address, stride of a sequence, of a token
         if x is None:
-            continue
-        # a dimension of one element may have any stride
-        if x.device != device or x.dtype != dtype or x.shape != (B, T, heads, 128) or x.stride(3) != 1 or (heads > 1 and x.stride(2) != 128):
-            raise ValueError("%s: expected %s [%d, %d, %d, 128] on %s with contiguous heads, got %s %s, strides %s, on %s" % (
-                name, dtype, B, T, heads, device, x.dtype, tuple(x.shape), x.stride(), x.device))
-        setattr(c, name + "_seq_stride", x.stride(0) if B > 1 else 0)
-        setattr(c, name + "_token_stride", x.stride(1) if T > 1 else 0)
-    ptr = lambda x: None if x is None else x.data_ptr()  # noqa: E731
-    opt = lambda x, dt, shape: None if x is None else _on_device(x, device, dt, shape)  # noqa: E731
-    if inv_freq is not None and inv_freq.dim() != 1:
-        raise ValueError("inv_freq has one dimension, got %s" % (tuple(inv_freq.shape),))
-    out = (opt(q_out, dtype, (B * H, T, G, 128)), opt(k_out, dtype, (B * H, T, 128)), opt(v_out, dtype, (B * H, T, 128)))
-    wq, wk = opt(q_weight, dtype, (128,)), opt(k_weight, dtype, (128,))
-    freq, pos = opt(inv_freq, torch.float32, inv_freq.shape if inv_freq is not None else None), _on_device(positions, device, torch.int32, (B, T))
-    lib = load()
-    with _on(device) as stream:
-        _check(lib.dynakv_norm_rope(C.byref(c), ptr(q), ptr(k), ptr(v), wq, wk, freq, pos, *out, stream), "dynakv_norm_rope")
+            return None, 0, 0
+        st = x.stride()
+        # (a dimension of one element may have any stride)
+        if x.get_device() != index or x.dtype is not dtype or x.shape != (B, T, n, 128) or st[3] != 1 or (st[2] != 128 and n > 1):
+            raise ValueError("%s: expected %s [%d, %d, %d, 128] on GPU %d with contiguous heads, got %s %s, strides %s, on %s" % (
+                name, dtype, B, T, n, index, x.dtype, tuple(x.shape), st, x.device))
+        return x.data_ptr(), st[0] if B > 1 else 0, st[1] if T > 1 else 0
+
+    qp, q0, q1 = rows(q, heads, "q")
+    kp, k0, k1 = rows(k, H, "k")
+    vp, v0, v1 = rows(v, H, "v")
+    pos = _on_device(positions, index, torch.int32, (B, T))
+    qo = None if q is None else _on_device(q_out, index, dtype, (B * H, T, G, 128))
+    ko = None if k is None else _on_device(k_out, index, dtype, (B * H, T, 128))
+    vo = None if v is None else _on_device(v_out, index, dtype, (B * H, T, 128))
+    wq = None if q_weight is None else _on_device(q_weight, index, dtype, (128,))
+    wk = None if k_weight is None else _on_device(k_weight, index, dtype, (128,))
+    pairs = 0 if inv_freq is None else inv_freq.numel()
+    freq = None if inv_freq is None else _on_device(inv_freq, index, torch.float32, (pairs,))
+    c = _Heads(_CODES[dtype], B, T, H, G, 128, 2 * pairs, 1 if interleaved else 0, eps, q0, q1, k0, k1, v0, v1)
+    _enqueue(index, "dynakv_norm_rope", load().dynakv_norm_rope, C.byref(c), qp, kp, vp, wq, wk, freq, pos, qo, ko, vo)
 
 
 def dynakv_tree_scratch_bytes(n_units: int, n_nodes: int, group_size: int) -> int:
@@ -244,17 +253,24 @@ def tree_scratch(n_units: int, n_nodes: int, group_size: int, device="cuda:0") -
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _tree_operands(device, dtype, U, Q, k_tree, v_tree, tree, out, lse, scratch):
-    """Addresses of what the two attentions of drafted tokens share, in the order of their arguments around the scale."""
+def _tree_operands(index, dtype, U, Q, k_tree, v_tree, tree, out, lse, scratch):
+    """Addresses of what the two attentions of drafted tokens share: (sizes and queries to tree), (out to scratch)."""
     if Q.dim() != 4 or (k_tree is None) != (v_tree is None):
         raise ValueError("Q is [units, nodes, query heads, 128]; drafted keys and values come together")
-    T, G = Q.shape[1], Q.shape[2]
-    opt = lambda x, dt, shape: None if x is None else _on_device(x, device, dt, shape)  # noqa: E731
-    q, o = _on_device(Q, device, dtype, (U, T, G, 128)), _on_device(out, device, dtype, (U, T, G, 128))
-    if scratch.device != device or scratch.dtype != torch.uint8 or not scratch.is_contiguous():
-        raise ValueError("scratch: expected contiguous bytes on %s" % device)
-    return (T, G, q, opt(k_tree, dtype, (U, T, 128)), opt(v_tree, dtype, (U, T, 128)), opt(tree, torch.int64, (U, T)), o,
-            opt(lse, torch.float32, (U, T, G)), scratch.data_ptr(), scratch.numel())
+    _, T, G, _ = shape = Q.shape
+    if shape[0] != U or shape[3] != 128:
+        raise ValueError("Q: expected [%d, nodes, query heads, 128], got %s" % (U, tuple(shape)))
+    q, o = _on_device(Q, index, dtype, shape), _on_device(out, index, dtype, shape)
+    k = v = t = l = None
+    if k_tree is not None:
+        k, v = _on_device(k_tree, index, dtype, (U, T, 128)), _on_device(v_tree, index, dtype, (U, T, 128))
+    if tree is not None:
+        t = _on_device(tree, index, torch.int64, (U, T))
+    if lse is not None:
+        l = _on_device(lse, index, torch.float32, (U, T, G))
+    if scratch.get_device() != index or scratch.dtype is not torch.uint8 or not scratch.is_contiguous():
+        raise ValueError("scratch: expected contiguous bytes on GPU %d" % index)
+    return T, G, (q, k, v, t), (o, l, scratch.data_ptr(), scratch.numel())
 
 
 class PackedCache:
@@ -263,16 +279,16 @@ class PackedCache:
 
     def __init__(self, k_codes, k_scales, v_codes, v_scales, dtype: str):
         self._lib = load()
-        self.device = _gpu(k_codes)
+        self.index = _gpu(k_codes)
         if k_codes.dim() != 3 or k_codes.shape[2] not in (128, 64) or dtype not in DTYPES:
             raise ValueError("codes are [units, capacity, 128 or 64] of dtype f32, f16 or bf16, got %s, %s" % (tuple(k_codes.shape), dtype))
         U, cap, width = k_codes.shape
         self.n_units, self.capacity, self.bits, self.dtype = U, cap, width // 16, TORCH_DTYPES[dtype]
         u8 = torch.uint8
         self.tensors = (k_codes, k_scales, v_codes, v_scales)
-        self._c = _Packed(U, cap, 128, DTYPES[dtype], self.bits, _on_device(k_codes, self.device, u8, (U, cap, width)),
-                          _on_device(k_scales, self.device, u8, (U, cap, 4)), _on_device(v_codes, self.device, u8, (U, cap, width)),
-                          _on_device(v_scales, self.device, u8, (U, cap, 4)))
+        self._c = _Packed(U, cap, 128, DTYPES[dtype], self.bits, _on_device(k_codes, self.index, u8, (U, cap, width)),
+                          _on_device(k_scales, self.index, u8, (U, cap, 4)), _on_device(v_codes, self.index, u8, (U, cap, width)),
+                          _on_device(v_scales, self.index, u8, (U, cap, 4)))
         self._ref = C.byref(self._c)
 
     @classmethod
@@ -286,30 +302,31 @@ class PackedCache:
         if K.dim() != 3:
             raise ValueError("rows are [units, tokens, 128], got %s" % (tuple(K.shape),))
         n = K.shape[1]
-        return n, _on_device(K, self.device, self.dtype, (self.n_units, n, 128)), _on_device(V, self.device, self.dtype, (self.n_units, n, 128))
+        shape = (self.n_units, n, 128)
+        return n, _on_device(K, self.index, self.dtype, shape), _on_device(V, self.index, self.dtype, shape)
+
+    def _per_unit(self, t):
+        return None if t is None else _on_device(t, self.index, torch.int32, (self.n_units,))
 
     def dynakv_packed_write(self, K: torch.Tensor, V: torch.Tensor, start: torch.Tensor | None = None, count: torch.Tensor | None = None):
         """Row i < count[u] of K, V [U, n, 128] goes to position start[u] + i (int32 [U]; None: 0 and n)."""
         n, kp, vp = self._rows(K, V)
-        sp = None if start is None else _on_device(start, self.device, torch.int32, (self.n_units,))
-        cp = None if count is None else _on_device(count, self.device, torch.int32, (self.n_units,))
-        with _on(self.device) as stream:
-            _check(self._lib.dynakv_packed_write(self._ref, kp, vp, n, sp, cp, stream), "dynakv_packed_write")
+        _enqueue(self.index, "dynakv_packed_write", self._lib.dynakv_packed_write, self._ref, kp, vp, n, self._per_unit(start),
+                 self._per_unit(count))
 
     def dynakv_packed_read(self, positions: torch.Tensor | None, K: torch.Tensor, V: torch.Tensor):
         """The rows at positions (int32 [U, n]; None: the first n) into K, V [U, n, 128]."""
         n, kp, vp = self._rows(K, V)
-        pp = None if positions is None else _on_device(positions, self.device, torch.int32, (self.n_units, n))
-        with _on(self.device) as stream:
-            _check(self._lib.dynakv_packed_read(self._ref, pp, n, kp, vp, stream), "dynakv_packed_read")
+        pp = None if positions is None else _on_device(positions, self.index, torch.int32, (self.n_units, n))
+        _enqueue(self.index, "dynakv_packed_read", self._lib.dynakv_packed_read, self._ref, pp, n, kp, vp)
 
     def dynakv_packed_attend(self, lengths, Q, k_tree, v_tree, tree, out, lse, scratch, softmax_scale: float = 0.0):
         """Attention of a tree of drafted tokens over rows 0..lengths[u]-1 (int32 [U]; None: all); operands as those of
         Index.dynakv_attend_tree."""
-        lp = None if lengths is None else _on_device(lengths, self.device, torch.int32, (self.n_units,))
-        T, G, q, k, v, t, o, l, s, n = _tree_operands(self.device, self.dtype, self.n_units, Q, k_tree, v_tree, tree, out, lse, scratch)
-        with _on(self.device) as stream:
-            _check(self._lib.dynakv_packed_attend(self._ref, lp, q, T, G, k, v, t, softmax_scale, o, l, s, n, stream), "dynakv_packed_attend")
+        T, G, before, after = _tree_operands(self.index, self.dtype, self.n_units, Q, k_tree, v_tree, tree, out, lse, scratch)
+        q, k, v, t = before
+        _enqueue(self.index, "dynakv_packed_attend", self._lib.dynakv_packed_attend, self._ref, self._per_unit(lengths), q, T, G, k, v, t,
+                 softmax_scale, *after)
 
 
 class Index:
@@ -409,11 +426,12 @@ class Index:
 
         Q, out [U, nodes, G, 128]; k_tree, v_tree [U, nodes, 128] or None; tree int64 [U, nodes] of which bit j says that the
         node sees drafted token j, or None: a chain; lse float32 [U, nodes, G] or None; scratch: tree_scratch(U, nodes, G)."""
-        T, G, q, k, v, t, o, l, s, n = _tree_operands(self.workspace.device, self._tdtype, self.cfg.n_units, Q, k_tree, v_tree, tree, out, lse, scratch)
+        index = self.workspace.get_device()
+        T, G, before, after = _tree_operands(index, self._tdtype, self.cfg.n_units, Q, k_tree, v_tree, tree, out, lse, scratch)
         if G != self.cfg.group_size:
             raise ValueError("the index has %d query heads per unit, Q %d" % (self.cfg.group_size, G))
-        with _on(self.workspace.device) as stream:
-            _check(self._lib.dynakv_attend_tree(self._h, q, T, k, v, t, o, l, s, n, stream), "dynakv_attend_tree")
+        q, k, v, t = before
+        _enqueue(index, "dynakv_attend_tree", self._lib.dynakv_attend_tree, self._h, q, T, k, v, t, *after)
 
     def decode_step_ptrs(self, q_ptr: int, budget: int, out_ptr: int, lse_ptr: int, k_ptr: int, v_ptr: int, stream: int):
         """dynakv_decode_step on raw device addresses, without per-call tensor checks, for loops where
