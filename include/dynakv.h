@@ -325,7 +325,7 @@ dynakv_status_t dynakv_norm_rope(const dynakv_heads_t* heads, const void* q, con
  * NaN throughout.  4-bit codes lie two to a byte, the even one in the low half, in two's complement, like those of 8 bits. */
 typedef struct {
   int32_t n_units;     /* U >= 1                                                       */
-  int32_t capacity;    /* rows per unit, >= 1                                          */
+  int32_t capacity;    /* rows per unit, 1..2^30                                       */
   int32_t head_dim;    /* must be 128                                                  */
   int32_t dtype;       /* dynakv_dtype_t of what is written and read                    */
   int32_t bits;        /* 8 or 4                                                       */

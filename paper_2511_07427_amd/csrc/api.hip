@@ -412,7 +412,7 @@ dynakv_status_t dynakv_norm_rope(const dynakv_heads_t* heads, const void* q, con
 }
 
 static bool packed_ok(const dynakv_packed_t* c) {
-  return c && c->n_units >= 1 && c->capacity >= 1 && c->head_dim == kHeadDim && dtype_ok(c->dtype) && (c->bits == 8 || c->bits == 4) &&
+  return c && c->n_units >= 1 && c->capacity >= 1 && c->capacity <= (1 << 30) && c->head_dim == kHeadDim && dtype_ok(c->dtype) && (c->bits == 8 || c->bits == 4) &&
          c->k_codes && c->v_codes && c->k_scales && c->v_scales && aligned(c->k_codes, 16) && aligned(c->v_codes, 16) &&
          aligned(c->k_scales, 4) && aligned(c->v_scales, 4);
 }

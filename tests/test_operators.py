@@ -66,7 +66,7 @@ def _packed(**kw):
 
 
 def test_packed_calls_refuse_what_they_do_not_take(lib):
-    bad = (dict(n_units=0), dict(capacity=0), dict(head_dim=64), dict(dtype=3), dict(bits=2), dict(k_codes=None), dict(v_scales=None),
+    bad = (dict(n_units=0), dict(capacity=0), dict(capacity=(1 << 30) + 1), dict(head_dim=64), dict(dtype=3), dict(bits=2), dict(k_codes=None), dict(v_scales=None),
            dict(k_codes=FAKE + 8), dict(v_scales=FAKE + 2))
     for b in bad:
         c = C.byref(_packed(**b))
