@@ -78,20 +78,23 @@ __device__ __forceinline__ void exchange(T& x, T& y, bool upper) {
   else y = got;
 }
 
-// Workgroup (token, chunk of 16 a.per heads); each row of 16 lanes takes `per` heads, kBatch of them on their way at once.  All rows go the
+// Workgroup (16 / HP tokens, chunk of HP a.per heads); HP rows of 16 lanes belong to a token, each takes `per` heads, kBatch of them on their way
+// at once.  All rows go the
 // same way through the code, values too (their result is dropped): with branches and 64-bit address arithmetic per kind of row the kernel
 // had as much to issue as to move (191 us for 16384 tokens of 80 rows).
-template <int DT, int ORDER>
+template <int DT, int ORDER, int HP>
 __global__ __launch_bounds__(256) void norm_rope_kernel(HeadsArgs a) {
   using F = Four<DT>;
   typedef typename F::T T;
   constexpr int kBatch = 4;
   constexpr size_t kRowBytes = kHeadDim / 4 * sizeof(T);
   const dynakv_heads_t& c = a.c;
-  const int b = blockIdx.x / c.n_tokens, t = blockIdx.x % c.n_tokens;
-  const int pos = a.positions[blockIdx.x];
+  const int lane = threadIdx.x & 15, row = (threadIdx.x >> 4) % HP;
+  const int token = HP == 16 ? (int)blockIdx.x : (int)blockIdx.x * (16 / HP) + (int)(threadIdx.x >> 4) / HP;
+  if (HP < 16 && token >= c.n_seqs * c.n_tokens) return;
+  const int b = token / c.n_tokens, t = token % c.n_tokens;
+  const int pos = a.positions[token];
   if (pos < 0) return;
-  const int lane = threadIdx.x & 15, row = threadIdx.x >> 4;
   const int H = c.n_kv_heads, G = c.group_size, nq = H * G, heads = nq + 2 * H, rot = c.rotary_dim;
   const bool upper = lane >= 8;
   const bool turns = 8 * lane < rot;
@@ -122,13 +125,13 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(HeadsArgs a) {
     return x;
   };
 
-  const int h0 = blockIdx.y * 16 * a.per + row, h1 = min(heads, (int)(blockIdx.y + 1) * 16 * a.per);
+  const int h0 = blockIdx.y * HP * a.per + row, h1 = min(heads, (int)(blockIdx.y + 1) * HP * a.per);
   float cs[4], sn[4], w[2][8];
-  for (int hb = h0; hb < h1; hb += 16 * kBatch) {
+  for (int hb = h0; hb < h1; hb += HP * kBatch) {
     T lo[kBatch], hi[kBatch];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-      const Head x = head(hb + 16 * k, h1);
+      const Head x = head(hb + HP * k, h1);
       if (!x.ok) continue;
       lo[k] = ((const T*)x.from)[i0 / 4];
       hi[k] = ((const T*)x.from)[i1 / 4];
@@ -159,7 +162,7 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(HeadsArgs a) {
     }
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-      const Head d = head(hb + 16 * k, h1);
+      const Head d = head(hb + HP * k, h1);
       if (!d.ok) continue;
       T u = lo[k], v = hi[k];
       if (ORDER == kHalf) exchange(u, v, upper);
@@ -206,25 +209,32 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(HeadsArgs a) {
   }
 }
 
-template <int DT>
-hipError_t launch(const HeadsArgs& a, dim3 grid, hipStream_t st) {
-  const int order = a.c.interleaved || a.c.rotary_dim == 0 ? kNear : a.c.rotary_dim == kHeadDim ? kHalf : kApart;
-  if (order == kNear) norm_rope_kernel<DT, kNear><<<grid, 256, 0, st>>>(a);
-  else if (order == kHalf) norm_rope_kernel<DT, kHalf><<<grid, 256, 0, st>>>(a);
-  else norm_rope_kernel<DT, kApart><<<grid, 256, 0, st>>>(a);
+template <int DT, int ORDER>
+hipError_t launch(HeadsArgs& a, hipStream_t st) {
+  const int heads = a.c.n_kv_heads * (a.c.group_size + 2);
+  const long long tokens = (long long)a.c.n_seqs * a.c.n_tokens;
+  // Few tokens: one head to a row of lanes, so that the chip has work.  Many: the angles of a token are what its rows of lanes each work out, for
+  // kBatch heads or more, so few rows share a token (5664 tokens of 9 heads: 18.6 us with 16 rows each, 15.4 with 8, 12.3 with 4).
+  const bool many = tokens * ((heads + 15) / 16) > 2048;
+  const int hp = many ? (heads > 32 ? 16 : heads > 16 ? 8 : 4) : heads > 8 ? 16 : heads > 4 ? 8 : 4;
+  a.per = many ? 8 : 1;
+  const dim3 grid((unsigned)((tokens * hp + 15) / 16), (heads + hp * a.per - 1) / (hp * a.per));
+  if (hp == 16) norm_rope_kernel<DT, ORDER, 16><<<grid, 256, 0, st>>>(a);
+  else if (hp == 8) norm_rope_kernel<DT, ORDER, 8><<<grid, 256, 0, st>>>(a);
+  else norm_rope_kernel<DT, ORDER, 4><<<grid, 256, 0, st>>>(a);
   return hipGetLastError();
+}
+template <int DT>
+hipError_t launch_order(HeadsArgs& a, hipStream_t st) {
+  if (a.c.interleaved || a.c.rotary_dim == 0) return launch<DT, kNear>(a, st);
+  return a.c.rotary_dim == kHeadDim ? launch<DT, kHalf>(a, st) : launch<DT, kApart>(a, st);
 }
 
 }  // namespace
 
 hipError_t launch_norm_rope(const HeadsArgs& in, hipStream_t st) {
   HeadsArgs a = in;
-  const int heads = a.c.n_kv_heads * (a.c.group_size + 2);
-  const long long tokens = (long long)a.c.n_seqs * a.c.n_tokens;
-  // Few tokens: a workgroup for every 16 rows, so that the chip has work; many: the angles of a token are taken once for up to 128 rows.
-  a.per = tokens * ((heads + 15) / 16) <= 2048 ? 1 : 8;
-  const dim3 grid((unsigned)tokens, (heads + 16 * a.per - 1) / (16 * a.per));
-  return a.c.dtype == DYNAKV_F32 ? launch<DYNAKV_F32>(a, grid, st) : a.c.dtype == DYNAKV_F16 ? launch<DYNAKV_F16>(a, grid, st) : launch<DYNAKV_BF16>(a, grid, st);
+  return a.c.dtype == DYNAKV_F32 ? launch_order<DYNAKV_F32>(a, st) : a.c.dtype == DYNAKV_F16 ? launch_order<DYNAKV_F16>(a, st) : launch_order<DYNAKV_BF16>(a, st);
 }
 
 }  // namespace dynakv

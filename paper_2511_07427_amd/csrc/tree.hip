@@ -814,7 +814,10 @@ hipError_t launch(TreeArgs a, hipStream_t st) {
   a.least = p.least;
   const hipError_t e = a.pages ? launch_source<DT, kList>(a, st) : a.cache.bits == 8 ? launch_source<DT, kPacked8>(a, st) : launch_source<DT, kPacked4>(a, st);
   if (e != hipSuccess || a.pieces == a.U) return e;
-  if (a.pieces > 8 * a.U) tree_join_kernel<DT, 8><<<(unsigned)((long long)a.U * R), 256, 0, st>>>(a);
+  // Few rows of many pieces: eight groups of lanes to a row; else one (4992 rows of 6 pieces 12 us with eight, 64 rows of 32 pieces 52 with one
+  // that takes a piece at a time).
+  const int each = min(a.pieces - a.U + 1, a.most / a.least + 1);
+  if (each > 8 && (long long)a.U * R <= 2048) tree_join_kernel<DT, 8><<<(unsigned)((long long)a.U * R), 256, 0, st>>>(a);
   else tree_join_kernel<DT, 1><<<(unsigned)(((long long)a.U * R + 7) / 8), 256, 0, st>>>(a);
   return hipGetLastError();
 }

@@ -173,7 +173,8 @@ def _outputs(dt, B, T, H, G, fill=7.0):
 @pytest.mark.parametrize("B,T,H,G,rot,interleaved,norm", [
     (1, 1, 8, 4, 128, False, True), (3, 5, 2, 7, 128, True, True), (2, 33, 1, 1, 64, False, True), (5, 2, 3, 16, 96, True, False),
     (1, 129, 4, 3, 8, False, False), (2, 7, 5, 2, 0, False, True), (1, 3, 7, 6, 120, False, True), (300, 1, 2, 4, 128, False, True),
-    (2, 700, 1, 5, 32, True, True)])
+    (2, 700, 1, 5, 32, True, True), (3, 701, 1, 3, 128, False, True), (1, 2100, 1, 1, 32, False, True), (2, 1100, 2, 9, 64, False, True),
+    (1, 1500, 4, 8, 128, False, True), (1, 401, 16, 8, 128, True, True), (1, 2, 16, 16, 96, False, True)])
 def test_norm_rope(dt, B, T, H, G, rot, interleaved, norm):
     gen = torch.Generator(DEV).manual_seed(B * 1000 + T)
     q, k, v = _fused_rows(dt, B, T, H, G, gen)
@@ -440,7 +441,8 @@ def _drafts(dt, U, T, G, gen, scale=1.0):
 @gpu
 @pytest.mark.parametrize("dt,bits", [("f16", 8), ("f16", 4), ("bf16", 8), ("bf16", 4), ("f32", 8), ("f32", 4)])
 @pytest.mark.parametrize("U,T,G,cap", [(1, 1, 1, 1), (3, 1, 8, 700), (2, 5, 4, 95), (5, 33, 3, 300), (2, 64, 16, 1500), (1, 64, 1, 64),
-                                       (40, 7, 7, 129), (2, 17, 2, 4096), (300, 2, 1, 40)])
+                                       (40, 7, 7, 129), (2, 17, 2, 4096), (300, 2, 1, 40),
+                                       (600, 1, 2, 90), (100, 4, 4, 2000), (9, 3, 16, 9000), (130, 9, 4, 700)])
 def test_packed_attention(dt, bits, U, T, G, cap):
     gen = torch.Generator(DEV).manual_seed(U + T + cap)
     K, V = (torch.randn(U, cap, D, generator=gen, device=DEV).to(TORCH_DTYPES[dt]) for _ in range(2))
