@@ -337,7 +337,7 @@ typedef struct {
 
 /* Quantises rows into a packed cache: row i < count[u] of unit u goes to position start[u] + i; one whose position lies
  * outside 0..capacity-1 is dropped.
- *   K, V   device, [U][n_tokens][head_dim] in cache->dtype; U * n_tokens < 2^31
+ *   K, V   device, [U][n_tokens][head_dim] in cache->dtype; U * n_tokens < 2^31, n_tokens = 0: nothing to do
  *   start  device, int32 [U], or null: 0
  *   count  device, int32 [U], or null: n_tokens (larger ones count as n_tokens) */
 dynakv_status_t dynakv_packed_write(const dynakv_packed_t* cache, const void* K, const void* V, int32_t n_tokens,

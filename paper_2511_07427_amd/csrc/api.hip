@@ -419,16 +419,16 @@ static bool packed_ok(const dynakv_packed_t* c) {
 
 dynakv_status_t dynakv_packed_write(const dynakv_packed_t* cache, const void* K, const void* V, int32_t n_tokens, const int32_t* start,
                                     const int32_t* count, void* stream) {
+  if (packed_ok(cache) && n_tokens == 0) return DYNAKV_OK;
   if (!packed_ok(cache) || !K || !V || n_tokens < 0 || !aligned(K, 16) || !aligned(V, 16) || !aligned(start, 4) || !aligned(count, 4)) return DYNAKV_EINVAL;
   if ((long long)cache->n_units * n_tokens >= (1ll << 31)) return DYNAKV_EINVAL;
-  if (n_tokens == 0) return DYNAKV_OK;
   return launch_packed_write(*cache, K, V, n_tokens, start, count, (hipStream_t)stream) == hipSuccess ? DYNAKV_OK : DYNAKV_EHIP;
 }
 
 dynakv_status_t dynakv_packed_read(const dynakv_packed_t* cache, const int32_t* positions, int32_t n, void* K, void* V, void* stream) {
+  if (packed_ok(cache) && n == 0) return DYNAKV_OK;
   if (!packed_ok(cache) || !K || !V || n < 0 || !aligned(K, 16) || !aligned(V, 16) || !aligned(positions, 4)) return DYNAKV_EINVAL;
   if ((long long)cache->n_units * n >= (1ll << 31)) return DYNAKV_EINVAL;
-  if (n == 0) return DYNAKV_OK;
   return launch_packed_read(*cache, positions, n, K, V, (hipStream_t)stream) == hipSuccess ? DYNAKV_OK : DYNAKV_EHIP;
 }
 

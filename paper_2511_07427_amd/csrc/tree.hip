@@ -167,7 +167,7 @@ struct Mma<DYNAKV_F32> {
 
 // Running state of a wavefront's 32 rows: lane l has row l % 32, register i of o[d] column 32 d + entry_of(i, l / 32).
 struct Rows {
-  float m, l;                                        // log2 domain; l of the lane's half of the entries
+  float m, l;                                        // what the weights are relative to (log2), and their sum over the lane's half of the entries
   f16v o[4];
 };
 
@@ -185,9 +185,12 @@ __device__ __forceinline__ f16v begin_scores(const float* bias, int lane) {
 }
 // N tiles of 32 entries.  Of a tile of the cache every row sees the same slots, those with a bias of 0; of drafted tokens (their bias is 0) those
 // whose bit is set in `seen`.  Slots that hold nothing have zeros in K and V.
-// The accumulators are rescaled only when a maximum has grown by more than 2^8 since they were last: until then weights grow up to 2^8,
-// which no type minds, and 64 products per tile and row are saved in all but a few tiles.
+// The accumulators are rescaled only when a maximum has grown by more than 2^kLazy since they last were: until then weights grow up to that,
+// and 64 products per tile and row are saved in all but a few tiles.  Weights are relative to 2^-kShift times the maximum: those of float16, whose
+// smallest step is 2^-24, so reach down to 2^-31 of the largest (many small ones beside a large one count), and stay below 2^15.
 constexpr float kLazy = 8.f;
+template <int DT>
+constexpr float kShift = DT == DYNAKV_F16 ? 7.f : 0.f;
 template <int DT, int N>
 __device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, const float* bias, const typename Mma<DT>::Q& q, bool drafts, unsigned long long seen, float sc,
                                         int lane) {
@@ -213,8 +216,8 @@ __device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, 
     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[n][i]);
   const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
   mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * sc;
-  if (__any(mx > st.m + kLazy)) {                    // (from -inf: any finite one)
-    const float mn = fmaxf(st.m, mx), alpha = mn == st.m ? 1.f : __builtin_amdgcn_exp2f(st.m - mn);
+  if (__any(mx > st.m + (kLazy + kShift<DT>))) {     // (from -inf: any finite one)
+    const float mn = fmaxf(st.m, mx - kShift<DT>), alpha = mn == st.m ? 1.f : __builtin_amdgcn_exp2f(st.m - mn);
     st.m = mn;
     st.l *= alpha;
 #pragma unroll
@@ -825,9 +828,9 @@ hipError_t launch(TreeArgs a, hipStream_t st) {
 // Scratch: where the pieces of each unit are, then a partial result of every row for each piece.  The most that any plan has.
 size_t where_bytes(int U) { return ((size_t)U * 8 + 255) & ~(size_t)255; }
 size_t part_bytes(int dtype, int U, int R) {
-  int most = 0;
-  for (int s = 1; may_share(dtype, U, R) && s <= 64; ++s) most = max(most, pieces_for(dtype, U, R, s));
-  return (size_t)most * R * kPartRow * sizeof(float);
+  if (!may_share(dtype, U, R)) return 0;
+  const int most = kMostRounds * kWorkgroups / row_blocks(dtype, R);
+  return (size_t)(most > U ? most : U) * R * kPartRow * sizeof(float);
 }
 
 }  // namespace

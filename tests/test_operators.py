@@ -628,6 +628,54 @@ def test_attention_of_large_and_equal_logits(dt):
 
 
 @gpu
+@pytest.mark.parametrize("dt,tiny", [("f16", 2.0 ** -20), ("bf16", 2.0 ** -120), ("f32", 2.0 ** -120)])
+def test_attention_keeps_small_values(dt, tiny):
+    # float16 values below its normal range, and small ones of the others, as keys and values of entries and drafts
+    U, T, G, cap = 2, 3, 4, 90
+    gen = torch.Generator(DEV).manual_seed(14)
+    Q, K1, V1, out, lse = _drafts(dt, U, T, G, gen)
+    K, V = (torch.randn(U, cap, D, generator=gen, device=DEV).to(TORCH_DTYPES[dt]) for _ in range(2))
+    V, V1, K1 = (V.float() * tiny).to(V.dtype), (V1.float() * tiny).to(V.dtype), (K1.float() * tiny).to(V.dtype)
+    c = PackedCache.zeros(U, cap, dt, 8, DEV)
+    c.dynakv_packed_write(K, V)
+    c.dynakv_packed_read(None, K, V)
+    c.dynakv_packed_attend(None, Q, K1, V1, None, out, None, tree_scratch(U, T, G, DEV))
+    chain = torch.ones(T, T, dtype=torch.bool, device=DEV).tril()
+    for u in range(U):
+        ref = _plain_tree(Q[u].double(), K[u].double(), V[u].double(), K1[u].double(), V1[u].double(), chain, D ** -0.5)
+        # relative to the weighted sum of |v|: weights to 2 h (their rounding and that of products below the type's normal range), and half a
+        # step of the smallest values there are for the output
+        floor = {"f16": 2.0 ** -25, "bf16": 2.0 ** -134, "f32": 2.0 ** -149}[dt]
+        err = (out[u].double() - ref[0]).abs()
+        lim = ref[2] * (2 * HALF[dt] + 264 * U32 * ref[4][..., None] + 2.0 ** -20) + HALF[dt] * ref[0].abs() + floor
+        assert bool((err <= lim).all()), (err - lim).max().item()
+        assert out[u].any()
+
+
+@gpu
+@pytest.mark.parametrize("dt", ["f16", "bf16", "f32"])
+def test_many_small_weights_beside_a_large_one(dt):
+    # a sink whose weight is e^16 times that of each of 100 000 others: together they are worth a hundredth of it
+    n, G = 100001, 2
+    c = PackedCache.zeros(1, n, dt, 8, DEV)
+    K, V = (torch.zeros(1, n, D, dtype=TORCH_DTYPES[dt], device=DEV) for _ in range(2))
+    K[0, 777, 0] = 16.0
+    V[0, :, 1] = 1.0
+    V[0, 777, 1] = 0.0
+    c.dynakv_packed_write(K, V)
+    Q = torch.zeros(1, 1, G, D, dtype=K.dtype, device=DEV)
+    Q[..., 0] = 1.0
+    out, lse = torch.empty_like(Q), torch.empty(1, 1, G, device=DEV)
+    c.dynakv_packed_attend(None, Q, None, None, None, out, lse, tree_scratch(1, 1, G, DEV), softmax_scale=1.0)
+    small = (n - 1) * float(np.exp(-16.0))
+    # each small weight, e^-16 = 0.97 * 2^-23 of the largest, is off by at most half a step: relative h, in float16, whose steps are 2^-31 of the
+    # largest there, 2^-9; the output's rounding h
+    off = {"f16": 2.0 ** -9 + 2.0 ** -11, "bf16": 2.0 ** -7, "f32": 2.0 ** -18}[dt]
+    assert abs(out[0, 0, 0, 1].item() / (small / (1 + small)) - 1) <= off
+    assert abs(lse[0, 0, 0].item() - (16 + np.log1p(small))) <= 1e-5
+
+
+@gpu
 def test_attention_refusals_of_the_binding():
     c = PackedCache.zeros(2, 64, "f16", 8, DEV)
     gen = torch.Generator(DEV).manual_seed(1)
@@ -648,6 +696,8 @@ def test_attention_refusals_of_the_binding():
         tree_scratch(1, 65, 1, DEV)
     with pytest.raises(ValueError):
         c.dynakv_packed_write(K1, V1.float())
+    c.dynakv_packed_write(K1[:, :0], V1[:, :0])                              # nothing to do
+    c.dynakv_packed_read(None, K1[:, :0], V1[:, :0])
     with pytest.raises(ValueError):
         c.dynakv_packed_read(torch.zeros(2, 2, dtype=torch.int32, device=DEV), K1, V1)
     assert (out == 3.0).all() and (lse == 3.0).all()
