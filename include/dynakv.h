@@ -293,7 +293,7 @@ dynakv_status_t dynakv_import_state(dynakv_index_t* index, const dynakv_state_t*
 typedef struct {
   int32_t dtype;       /* dynakv_dtype_t of all rows and of the weights                              */
   int32_t n_seqs;      /* B >= 1                                                                    */
-  int32_t n_tokens;    /* T >= 1 per sequence; n_seqs * n_tokens * heads < 2^31                      */
+  int32_t n_tokens;    /* T >= 1 per sequence; n_seqs * n_tokens * H * (G + 2) < 2^27               */
   int32_t n_kv_heads;  /* H >= 1                                                                    */
   int32_t group_size;  /* G, query heads per KV head, 1..16                                         */
   int32_t head_dim;    /* must be 128                                                               */
@@ -337,14 +337,14 @@ typedef struct {
 
 /* Quantises rows into a packed cache: row i < count[u] of unit u goes to position start[u] + i; one whose position lies
  * outside 0..capacity-1 is dropped.
- *   K, V   device, [U][n_tokens][head_dim] in cache->dtype; U * n_tokens < 2^31, n_tokens = 0: nothing to do
+ *   K, V   device, [U][n_tokens][head_dim] in cache->dtype; U * n_tokens < 2^28, n_tokens = 0: nothing to do
  *   start  device, int32 [U], or null: 0
  *   count  device, int32 [U], or null: n_tokens (larger ones count as n_tokens) */
 dynakv_status_t dynakv_packed_write(const dynakv_packed_t* cache, const void* K, const void* V, int32_t n_tokens,
                                     const int32_t* start, const int32_t* count, void* stream);
 
-/* Reads rows of a packed cache back: K, V device, [U][n][head_dim] in cache->dtype; row i of unit u is the one at
- * positions[u][i].
+/* Reads rows of a packed cache back: K, V device, [U][n][head_dim] in cache->dtype, U * n < 2^28; row i of unit u is the one
+ * at positions[u][i].
  *   positions  device, int32 [U][n], or null: 0..n-1; where one lies outside 0..capacity-1 the output row is left as it is */
 dynakv_status_t dynakv_packed_read(const dynakv_packed_t* cache, const int32_t* positions, int32_t n, void* K, void* V,
                                    void* stream);
@@ -357,7 +357,7 @@ size_t dynakv_tree_scratch_bytes(int32_t n_units, int32_t n_nodes, int32_t group
  * last retrieval of the index gathered, one softmax over those and the drafted tokens each node sees:
  *   out[u][i][g] = softmax(scale * q . {gathered keys, K_tree[u][j] for the bits j of tree[u][i]}) . {values}
  * The index must not have changed since that retrieval (DYNAKV_ESTATE; a captured graph holds both calls), and does not change.
- *   Q               device, [U][n_nodes][G][head_dim] in cfg.dtype, 1 <= n_nodes <= 64
+ *   Q               device, [U][n_nodes][G][head_dim] in cfg.dtype, 1 <= n_nodes <= 64; U < 2^22, U * n_nodes * G < 2^28
  *   K_tree, V_tree  device, [U][n_nodes][head_dim] in cfg.dtype, or both null: the gathered entries alone
  *   tree            device, uint64 [U][n_nodes]: bit j: node i sees drafted token j (itself included where its bit is set; bits
  *                   from n_nodes on are ignored), or null: a chain, node i sees 0..i.  What a node does not see, NaN and

@@ -384,6 +384,11 @@ dynakv_status_t dynakv_import_state(dynakv_index_t* ix, const dynakv_state_t* sr
 
 // ---- operators beside the index ----------------------------------------------------------------------
 static bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+// A grid has fewer than 2^32 work-items: what keeps each of these kernels below that.  Norm + rotation: at most 64 / 3 work-items for a row
+// (few heads to a token); packed rows: 16 each; attention: 512 for every unit and every further 256 rows (float32: 256, 32 rows).
+constexpr unsigned kMaxHeadRows = 1u << 27;
+constexpr long long kMaxPackedRows = 1ll << 28, kMaxTreeRows = 1ll << 28;
+constexpr int kMaxTreeUnits = 1 << 22;
 static bool dtype_ok(int dtype) { return dtype == DYNAKV_F32 || dtype == DYNAKV_F16 || dtype == DYNAKV_BF16; }
 
 dynakv_status_t dynakv_norm_rope(const dynakv_heads_t* heads, const void* q, const void* k, const void* v, const void* q_weight,
@@ -397,7 +402,7 @@ dynakv_status_t dynakv_norm_rope(const dynakv_heads_t* heads, const void* q, con
   if (!(c.eps >= 0.f && c.eps <= 3.4e38f)) return DYNAKV_EINVAL;
   if ((!q) != (!Q) || (!k) != (!K) || (!v) != (!V)) return DYNAKV_EINVAL;
   const unsigned __int128 rows = (unsigned __int128)((unsigned long long)c.n_seqs * c.n_tokens) * ((unsigned long long)c.n_kv_heads * (c.group_size + 2));
-  if (rows >= ((unsigned __int128)1 << 31) || (long long)c.n_kv_heads * (c.group_size + 2) > (1 << 19)) return DYNAKV_EINVAL;
+  if (rows >= kMaxHeadRows || (long long)c.n_kv_heads * (c.group_size + 2) > (1 << 19)) return DYNAKV_EINVAL;
   const int64_t step = 16 / elem_size(c.dtype);
   const void* rows_of[] = {q, k, v, q_weight, k_weight, Q, K, V};
   for (const void* p : rows_of)
@@ -421,19 +426,21 @@ dynakv_status_t dynakv_packed_write(const dynakv_packed_t* cache, const void* K,
                                     const int32_t* count, void* stream) {
   if (packed_ok(cache) && n_tokens == 0) return DYNAKV_OK;
   if (!packed_ok(cache) || !K || !V || n_tokens < 0 || !aligned(K, 16) || !aligned(V, 16) || !aligned(start, 4) || !aligned(count, 4)) return DYNAKV_EINVAL;
-  if ((long long)cache->n_units * n_tokens >= (1ll << 31)) return DYNAKV_EINVAL;
+  if ((long long)cache->n_units * n_tokens >= kMaxPackedRows) return DYNAKV_EINVAL;
   return launch_packed_write(*cache, K, V, n_tokens, start, count, (hipStream_t)stream) == hipSuccess ? DYNAKV_OK : DYNAKV_EHIP;
 }
 
 dynakv_status_t dynakv_packed_read(const dynakv_packed_t* cache, const int32_t* positions, int32_t n, void* K, void* V, void* stream) {
   if (packed_ok(cache) && n == 0) return DYNAKV_OK;
   if (!packed_ok(cache) || !K || !V || n < 0 || !aligned(K, 16) || !aligned(V, 16) || !aligned(positions, 4)) return DYNAKV_EINVAL;
-  if ((long long)cache->n_units * n >= (1ll << 31)) return DYNAKV_EINVAL;
+  if ((long long)cache->n_units * n >= kMaxPackedRows) return DYNAKV_EINVAL;
   return launch_packed_read(*cache, positions, n, K, V, (hipStream_t)stream) == hipSuccess ? DYNAKV_OK : DYNAKV_EHIP;
 }
 
 size_t dynakv_tree_scratch_bytes(int32_t n_units, int32_t n_nodes, int32_t group_size) {
-  if (n_units < 1 || n_nodes < 1 || n_nodes > kMaxNodes || group_size < 1 || group_size > 16) return 0;
+  if (n_units < 1 || n_units >= kMaxTreeUnits || n_nodes < 1 || n_nodes > kMaxNodes || group_size < 1 || group_size > 16 ||
+      (long long)n_units * n_nodes * group_size >= kMaxTreeRows)
+    return 0;
   return tree_scratch_bytes(n_units, n_nodes, group_size);
 }
 
@@ -443,7 +450,7 @@ static dynakv_status_t tree_args(TreeArgs* a, int U, int T, int G, int dtype, fl
   if (!Q || !out || !scratch || (!K1) != (!V1) || T < 1 || T > kMaxNodes || G < 1 || G > 16) return DYNAKV_EINVAL;
   if (!aligned(Q, 16) || !aligned(K1, 16) || !aligned(V1, 16) || !aligned(out, 16) || !aligned(scratch, 16) || !aligned(tree, 8) || !aligned(lse, 4))
     return DYNAKV_EINVAL;
-  if ((long long)U * T * G >= (1ll << 31)) return DYNAKV_EINVAL;
+  if (U >= kMaxTreeUnits || (long long)U * T * G >= kMaxTreeRows) return DYNAKV_EINVAL;
   if (scratch_bytes < tree_scratch_bytes(U, T, G)) return DYNAKV_ECAPACITY;
   a->U = U; a->T = T; a->G = G; a->dtype = dtype;
   a->sc = scale * 1.4426950408889634f;

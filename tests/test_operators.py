@@ -36,7 +36,7 @@ FAKE = 1 << 20
 
 def _heads(**kw):
     c = dict(dtype=1, n_seqs=2, n_tokens=3, n_kv_heads=2, group_size=4, head_dim=128, rotary_dim=128, interleaved=0, eps=1e-6,
-             q_seq_stride=3072 * 8, q_token_stride=2048, k_seq_stride=2048, k_token_stride=256, v_seq_stride=2048, v_token_stride=256)
+             q_seq_stride=2048 * 8, q_token_stride=2048, k_seq_stride=2048, k_token_stride=256, v_seq_stride=2048, v_token_stride=256)
     c.update(kw)
     return binding._Heads(**c)
 
@@ -106,6 +106,21 @@ def test_attentions_of_drafted_tokens_refuse_what_they_do_not_take(lib):
     assert lib.dynakv_attend_tree(h, FAKE, 5, FAKE, None, FAKE, FAKE, FAKE, FAKE, need, None) == 1
     assert lib.dynakv_attend_tree(h, FAKE, 5, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, need - 1, None) == 2
     assert lib.dynakv_destroy(h) == 0
+
+
+def test_sizes_beyond_what_one_launch_holds_are_refused(lib):
+    """Fewer than 2^32 work-items to a launch."""
+    def heads(B, T, H, G):
+        c = _heads(n_seqs=B, n_tokens=T, n_kv_heads=H, group_size=G)
+        return lib.dynakv_norm_rope(C.byref(c), FAKE, FAKE, FAKE, FAKE, None, FAKE, FAKE, FAKE, FAKE, FAKE, None)
+    assert heads(1, (1 << 27) // 3 + 1, 1, 1) == 1 and heads(1 << 13, 1 << 13, 1, 2) == 1
+    c = C.byref(_packed(n_units=4, capacity=1 << 30))
+    assert lib.dynakv_packed_write(c, FAKE, FAKE, 1 << 26, None, None, None) == 1
+    assert lib.dynakv_packed_read(c, None, 1 << 26, FAKE, FAKE, None) == 1
+    for U, T, G in ((1 << 22, 1, 1), (1 << 18, 64, 16)):
+        assert lib.dynakv_tree_scratch_bytes(U, T, G) == 0
+        c = C.byref(_packed(n_units=U, capacity=1))
+        assert lib.dynakv_packed_attend(c, None, FAKE, T, G, None, None, None, 0.0, FAKE, None, FAKE, 1 << 62, None) == 1
 
 
 def test_structs_match_the_header():
@@ -464,6 +479,47 @@ def test_packed_attention(dt, bits, U, T, G, cap):
         n = max(0, int(lengths[u]))
         ref = _plain_tree(Q[u].double(), K[u, :n].double(), V[u, :n].double(), K1[u].double(), V1[u].double(), seen[u], D ** -0.5)
         _check_tree(out[u], lse[u], ref, dt, n + T)
+
+
+@gpu
+@pytest.mark.parametrize("dt,bits", [("f16", 8), ("f16", 4), ("bf16", 8), ("bf16", 4), ("f32", 8), ("f32", 4)])
+@pytest.mark.parametrize("T,G", [(1, 3), (20, 4)])
+def test_packed_attention_over_blocks_that_are_nan(dt, bits, T, G):
+    # a value that is not finite makes its block NaN: of a key for all who see it, of a value in the block's 32 columns alone
+    U, cap = 3, 200
+    gen = torch.Generator(DEV).manual_seed(31)
+    K, V = (torch.randn(U, cap, D, generator=gen, device=DEV).to(TORCH_DTYPES[dt]) for _ in range(2))
+    K[0, 77, 5], V[1, 120, 40] = float("inf"), float("nan")
+    c = PackedCache.zeros(U, cap, dt, bits, DEV)
+    c.dynakv_packed_write(K, V)
+    c.dynakv_packed_read(None, K, V)
+    assert K[0, 77, :32].isnan().all() and V[1, 120, 32:64].isnan().all() and K.isnan().sum() == 32 and V.isnan().sum() == 32
+    Q, K1, V1, out, lse = _drafts(dt, U, T, G, gen)
+    seen = _random_tree(U, T, gen)
+    c.dynakv_packed_attend(None, Q, K1, V1, _bits(seen), out, lse, tree_scratch(U, T, G, DEV))
+    assert out[0].isnan().all() and lse[0].isnan().all()
+    assert out[1, ..., 32:64].isnan().all()
+    out[1, ..., 32:64], V[1, :, 32:64], V1[1, :, 32:64] = 0, 0, 0
+    for u in (1, 2):
+        ref = _plain_tree(Q[u].double(), K[u].double(), V[u].double(), K1[u].double(), V1[u].double(), seen[u], D ** -0.5)
+        _check_tree(out[u], lse[u], ref, dt, cap + T)
+
+
+@gpu
+def test_packed_attention_of_a_unit_beyond_32_bits():
+    cap = (1 << 25) + 77                                        # the second unit's codes begin 4.3 GB into theirs
+    c = PackedCache.zeros(2, cap, "f16", 8, DEV)
+    gen = torch.Generator(DEV).manual_seed(4)
+    K, V = (torch.randn(2, 300, D, generator=gen, device=DEV).half() for _ in range(2))
+    c.dynakv_packed_write(K, V)
+    c.dynakv_packed_read(None, K, V)
+    lengths = torch.tensor([20, 300], dtype=torch.int32, device=DEV)
+    Q, K1, V1, out, lse = _drafts("f16", 2, 3, 4, gen)
+    c.dynakv_packed_attend(lengths, Q, K1, V1, None, out, lse, tree_scratch(2, 3, 4, DEV))
+    chain = torch.ones(3, 3, dtype=torch.bool, device=DEV).tril()
+    for u, n in enumerate((20, 300)):
+        ref = _plain_tree(Q[u].double(), K[u, :n].double(), V[u, :n].double(), K1[u].double(), V1[u].double(), chain, D ** -0.5)
+        _check_tree(out[u], lse[u], ref, "f16", n + 3)
 
 
 def _retrieved(dt, U, G, n, M, budget, seed, **more):
