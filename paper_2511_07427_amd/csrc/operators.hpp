@@ -47,7 +47,7 @@ struct TreeArgs {
   dynakv_packed_t cache;
   const int* lengths;
   // set by launch_tree
-  int RB;                                           // blocks of rows of a unit
+  int RB, rows;                                     // blocks of rows of a unit, rows of each
   int pieces;                                       // most workgroups for each; U: every unit whole
   int least;                                        // entries for which another workgroup is worth it
   int* where;                                       // [U][2] first piece and pieces of a unit

@@ -186,7 +186,7 @@ __device__ __forceinline__ f16v begin_scores(const float* bias, int lane) {
 // N tiles of 32 entries.  Of a tile of the cache every row sees the same slots, those with a bias of 0; of drafted tokens (their bias is 0) those
 // whose bit is set in `seen`.  Slots that hold nothing have zeros in K and V.
 // The accumulators are rescaled only when a maximum has grown by more than 2^kLazy since they last were: until then weights grow up to that,
-// and 64 products per tile and row are saved in all but a few tiles.  Weights are relative to 2^-kShift times the maximum: those of float16, whose
+// and 64 products per tile and row are saved in all but a few tiles (3 % of the time of 128 packed units of 128 rows).  Weights are relative to 2^-kShift times the maximum: those of float16, whose
 // smallest step is 2^-24, so reach down to 2^-31 of the largest (many small ones beside a large one count), and stay below 2^15.
 constexpr float kLazy = 8.f;
 template <int DT>
@@ -523,7 +523,8 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
   if (piece >= a.pieces) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int grp = wave / WR, wr = wave % WR;
-  const int R = a.T * a.G, row = (rb * WR + wr) * kSub + (lane & 31);
+  const int R = a.T * a.G, row = rb * a.rows + wr * kSub + (lane & 31);
+  const bool some = WR == 1 || (wr * kSub < a.rows && rb * a.rows + wr * kSub < R);      // else the wavefront only helps to load
   const Piece pc = piece_of<SRC>(a, piece, lane);
   if (pc.u < 0) return;
   const int u = __builtin_amdgcn_readfirstlane(pc.u), ns = __builtin_amdgcn_readfirstlane(pc.count), s = __builtin_amdgcn_readfirstlane(pc.s);
@@ -535,10 +536,11 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
     a.where[2 * u + 1] = ns;
   }
 
-  // the queries, the drafted tokens (the unit's last split; group g takes those from g kSlots on) and the first tile are requested together
+  // The queries, the drafted tokens and the first tile are requested together.  The drafted tokens are the unit's last piece's, there of the last
+  // groups, which have the fewest tiles (of the first ones: 20.3 us for a float32 unit of 256 entries and five tokens; so 15.3).
   typename M::Q q;
   M::load_q(q, a.Q, (size_t)u * R + min(row, R - 1), h);      // (rows beyond the last: its queries; not written)
-  const int r0 = wr * Sh::kMine, j0 = grp * kSlots;
+  const int r0 = wr * Sh::kMine, j0 = (kGroups - 1 - grp) * kSlots;
   const bool drafts = a.K1 && s == ns - 1, mine = drafts && j0 < a.T;
   unsigned long long word = 0;
   Drafts<DT, Sh::kMine> draft;
@@ -621,7 +623,7 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
       }
     };
     if constexpr (kLast) next();                     // into the other place
-    if (i < 0 ? mine : kGroups == 1 || t < t1)
+    if (some && (i < 0 ? mine : kGroups == 1 || t < t1))
       consume<DT, N>(st, kt, kt + Sh::kTileK, (const float*)(kt + Sh::kTileK + Sh::kTileV), q, i < 0, word, a.sc, lane);
     sync();
     if constexpr (!kLast) {
@@ -669,8 +671,8 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
   }
   lds_barrier();
   for (int i = threadIdx.x; i < WR * kSub * (kHeadDim / 4); i += Sh::kThreads) {
-    const int r = i >> 5, c = (i & 31) * 4, rr = rb * WR * kSub + r;      // row r of the workgroup: wavefront r / 32 of every group
-    if (rr >= R) break;
+    const int r = i >> 5, c = (i & 31) * 4, rr = rb * a.rows + r;      // row r of the workgroup: wavefront r / 32 of every group
+    if (r >= a.rows || rr >= R) break;
     float mw[kGroups], m = -__builtin_inff(), l = 0.f;
 #pragma unroll
     for (int w = 0; w < kGroups; ++w) { mw[w] = mo[(w * WR * kSub + r) * kOut + kHeadDim]; m = fmaxf(m, mw[w]); }
@@ -753,13 +755,18 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   if (a.lse && c == 0) a.lse[i] = none ? m : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// Wavefronts of a workgroup that take rows of their own, up to eight times 32 of the R rows of a unit.
+// Wavefronts of a workgroup that take rows of their own, up to eight times 32 of the R rows of a unit: what they read of LDS they share with none,
+// what they load and unpack with all.  R = 427, 2048 entries of 112 units: 171 us with one, 147 with two, 108 with four, 92 with eight; R = 128 of
+// 128 packed units: 136, 108, 69 with four.  For 32 rows a second wavefront would be idle: 8 long packed units 62 us, with two 78.  Several blocks of
+// rows are made alike (R = 427: seven wavefronts of eight twice, 88 us, instead of eight and six, 92).  A float32 wavefront's queries and sums
+// leave room for one on a SIMD; its matrix instructions are what bounds it, whoever loads the tiles.
 int row_waves(int dtype, int R) { return dtype == DYNAKV_F32 || R <= kSub ? 1 : R <= 2 * kSub ? 2 : R <= 4 * kSub ? 4 : 8; }
 
 // Workgroups that a call gets for each block of rows (`pieces`), and the fewest entries for which another one is worth it (`least`), from a
 // model in ns, measured on 1 to 256 units: 256 workgroups run at once; one takes 9 us to begin and end, and per entry the larger of its
 // bytes (at its share of 5 TB/s, at most 64 per ns) and the work of its rows; the kernel that joins takes 6 us.  Units of one length would be
-// cut into s pieces each; a multiple of 256 workgroups that has room for those is what units of any lengths share.
+// cut into s pieces each; a multiple of 256 workgroups that has room for those is what units of any lengths share.  (8 units of 131072 packed
+// entries: 62 us, whole 1247; 128 units of up to 8191: 69, whole 146.)
 struct Plan { int pieces, least; };
 constexpr int kMostRounds = 4;                       // bounds the scratch
 int row_blocks(int dtype, int R) { return (R + row_waves(dtype, R) * kSub - 1) / (row_waves(dtype, R) * kSub); }
@@ -792,6 +799,7 @@ hipError_t launch_shape(TreeArgs& a, hipStream_t st) {
   using Sh = Shape<DT, SRC, WR>;
   const int R = a.T * a.G;
   a.RB = (R + WR * kSub - 1) / (WR * kSub);
+  a.rows = ((R + kSub - 1) / kSub + a.RB - 1) / a.RB * kSub;
   tree_kernel<DT, SRC, WR><<<(unsigned)((a.pieces + 7ll) / 8 * 8 * a.RB), Sh::kThreads, Sh::kLds, st>>>(a);
   return hipGetLastError();
 }
