@@ -26,7 +26,7 @@ __device__ __forceinline__ float row16_sum(float x) {
 
 // How a lane's eight elements of a row lie: kNear: 8 l .. 8 l + 7 (neighbouring pairs, or no rotation); kHalf: the whole head is rotated in pairs
 // 64 apart: the lane loads those eight too, and lanes l and l + 8 exchange four of them; kApart: other pairs rotary_dim / 2 apart: two runs of four,
-// loaded as they are needed (8-byte loads move 7 % less than 16-byte loads and the exchange).
+// loaded as they are needed (16384 tokens of 80 bfloat16 rows: 160 us so, 148 with the exchange).
 enum Order { kNear, kHalf, kApart };
 
 // Four elements as they lie in memory.
@@ -79,10 +79,9 @@ __device__ __forceinline__ void exchange(T& x, T& y, bool upper) {
 }
 
 // Workgroup (16 / HP tokens, chunk of HP a.per heads); HP rows of 16 lanes belong to a token, each takes `per` heads, kBatch of them on their way
-// at once.  All rows go the
-// same way through the code, values too (their result is dropped): with branches and 64-bit address arithmetic per kind of row the kernel
-// had as much to issue as to move (191 us for 16384 tokens of 80 rows).
-template <int DT, int ORDER, int HP>
+// at once.  All rows go the same way through the code, values too (their result is dropped): with branches and 64-bit address arithmetic per
+// kind of row the kernel had as much to issue as to move (191 us for 16384 tokens of 80 bfloat16 rows; now 145 to 153, 4.4 to 4.6 TB/s).
+template <int DT, int ORDER, int HP, bool STREAM>
 __global__ __launch_bounds__(256) void norm_rope_kernel(HeadsArgs a) {
   using F = Four<DT>;
   typedef typename F::T T;
@@ -133,8 +132,8 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(HeadsArgs a) {
     for (int k = 0; k < kBatch; ++k) {
       const Head x = head(hb + HP * k, h1);
       if (!x.ok) continue;
-      lo[k] = ((const T*)x.from)[i0 / 4];
-      hi[k] = ((const T*)x.from)[i1 / 4];
+      lo[k] = get<STREAM>((const T*)x.from + i0 / 4);
+      hi[k] = get<STREAM>((const T*)x.from + i1 / 4);
     }
     if (hb == h0) {                                  // while the first rows are on their way
 #pragma unroll
@@ -203,25 +202,34 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(HeadsArgs a) {
       u = F::put(x);
       v = F::put(y);
       if (ORDER == kHalf) exchange(u, v, upper);
-      ((T*)d.to)[i0 / 4] = d.isv ? lo[k] : u;
-      ((T*)d.to)[i1 / 4] = d.isv ? hi[k] : v;
+      put<STREAM>((T*)d.to + i0 / 4, d.isv ? lo[k] : u);
+      put<STREAM>((T*)d.to + i1 / 4, d.isv ? hi[k] : v);
     }
   }
+}
+
+// Past the caches where rows in and out are more than they hold (80 rows of bfloat16 a token: 16384 tokens 148 us, so 142; 8192: 76, 70; but
+// 4096, 160 MB: 35, 39, and with a kernel that reads the queries after it 54, 65).
+template <int DT, int ORDER, int HP>
+void launch_rows(const HeadsArgs& a, dim3 grid, hipStream_t st) {
+  const long long rows = (long long)a.c.n_seqs * a.c.n_tokens * a.c.n_kv_heads * ((a.q ? a.c.group_size : 0) + (a.k ? 1 : 0) + (a.v ? 1 : 0));
+  if (2 * rows * kHeadDim * elem_size(DT) > kCacheBytes) norm_rope_kernel<DT, ORDER, HP, true><<<grid, 256, 0, st>>>(a);
+  else norm_rope_kernel<DT, ORDER, HP, false><<<grid, 256, 0, st>>>(a);
 }
 
 template <int DT, int ORDER>
 hipError_t launch(HeadsArgs& a, hipStream_t st) {
   const int heads = a.c.n_kv_heads * (a.c.group_size + 2);
   const long long tokens = (long long)a.c.n_seqs * a.c.n_tokens;
-  // Few tokens: one head to a row of lanes, so that the chip has work.  Many: the angles of a token are what its rows of lanes each work out, for
+  // Few tokens: one head to a row of lanes, so that the chip has work (one token of 48 rows 3.9 us, as many would be 4.2).  Many: the angles of a token are what its rows of lanes each work out, for
   // kBatch heads or more, so few rows share a token (5664 tokens of 9 heads: 18.6 us with 16 rows each, 15.4 with 8, 12.3 with 4).
   const bool many = tokens * ((heads + 15) / 16) > 2048;
   const int hp = many ? (heads > 32 ? 16 : heads > 16 ? 8 : 4) : heads > 8 ? 16 : heads > 4 ? 8 : 4;
   a.per = many ? 8 : 1;
   const dim3 grid((unsigned)((tokens * hp + 15) / 16), (heads + hp * a.per - 1) / (hp * a.per));
-  if (hp == 16) norm_rope_kernel<DT, ORDER, 16><<<grid, 256, 0, st>>>(a);
-  else if (hp == 8) norm_rope_kernel<DT, ORDER, 8><<<grid, 256, 0, st>>>(a);
-  else norm_rope_kernel<DT, ORDER, 4><<<grid, 256, 0, st>>>(a);
+  if (hp == 16) launch_rows<DT, ORDER, 16>(a, grid, st);
+  else if (hp == 8) launch_rows<DT, ORDER, 8>(a, grid, st);
+  else launch_rows<DT, ORDER, 4>(a, grid, st);
   return hipGetLastError();
 }
 template <int DT>

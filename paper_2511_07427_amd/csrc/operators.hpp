@@ -5,6 +5,20 @@
 
 namespace dynakv {
 
+// Calls that move more than the memory-side cache holds leave nothing in it that a later one could find: they load and store past the caches
+// (STREAM), so that what is there of others stays.  Smaller calls do not, for the kernel that reads their rows next.
+constexpr long long kCacheBytes = 256ll << 20;
+template <bool STREAM, class T>
+__device__ __forceinline__ T get(const T* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+template <bool STREAM, class T>
+__device__ __forceinline__ void put(T* p, T x) {
+  if constexpr (STREAM) __builtin_nontemporal_store(x, p);
+  else *p = x;
+}
+
 struct HeadsArgs {
   dynakv_heads_t c;
   const void *q, *k, *v, *wq, *wk;

@@ -394,6 +394,53 @@ def test_packed_offsets_beyond_32_bits():
     assert bool(((lse[0, 0].double() - den.log()).abs() <= 1e-4).all())     # 3e7 terms of a float32 sum in 32-entry and wavefront parts
 
 
+# ----------------------------------------------------------------------------------------------- calls beyond the caches
+# More than 256 MiB: the kernels' accesses go past the caches there.  The rows are those of calls on parts of them, to the bit.
+@gpu
+@pytest.mark.parametrize("dt,T,H,G,rot,interleaved", [("bf16", 6601, 8, 8, 128, False), ("f16", 45003, 2, 4, 64, False), ("f32", 13305, 4, 3, 96, True)])
+def test_norm_rope_of_more_than_the_caches_hold(dt, T, H, G, rot, interleaved):
+    t = TORCH_DTYPES[dt]
+    gen = torch.Generator(DEV).manual_seed(T)
+    x = torch.randn(1, T, (G + 2) * H, D, generator=gen, device=DEV).to(t)
+    assert 2 * x.numel() * x.element_size() > 256 << 20
+    w = (1 + 0.1 * torch.randn(D, generator=gen, device=DEV)).to(t)
+    freq = torch.rand(rot // 2, generator=gen, device=DEV)
+    pos = torch.arange(T, dtype=torch.int32, device=DEV)[None].contiguous()
+    pos[0, T // 3] = -1
+
+    def call(a, b):
+        rows, n = x[:, a:b], b - a
+        out = [torch.full(s, 3.0, dtype=t, device=DEV) for s in ((H, n, G, D), (H, n, D), (H, n, D))]
+        dynakv_norm_rope(rows[:, :, :H * G], rows[:, :, H * G:H * G + H], rows[:, :, H * G + H:], pos[:, a:b].contiguous(), *out, w, w, freq,
+                         interleaved=interleaved)
+        return out
+    whole, step = call(0, T), T // 3 + 1
+    for a in range(0, T, step):
+        for got, want in zip(whole, call(a, min(T, a + step))):
+            assert torch.equal(got[:, a:a + step], want)
+
+
+@gpu
+@pytest.mark.parametrize("dt,bits,n", [("bf16", 8, 33001), ("f16", 4, 33001), ("f32", 8, 16501), ("f32", 4, 16501), ("bf16", 4, 33001), ("f16", 8, 33001)])
+def test_packed_rows_of_more_than_the_caches_hold(dt, bits, n):
+    U, step, gen = 16, n // 3 + 1, torch.Generator(DEV).manual_seed(n)
+    K, V = (torch.randn(U, n, D, generator=gen, device=DEV).to(TORCH_DTYPES[dt]) for _ in range(2))
+    assert 2 * K.numel() * K.element_size() > 256 << 20
+    whole, parts = PackedCache.zeros(U, n, dt, bits, DEV), PackedCache.zeros(U, n, dt, bits, DEV)
+    whole.dynakv_packed_write(K, V)
+    for a in range(0, n, step):
+        parts.dynakv_packed_write(K[:, a:a + step].contiguous(), V[:, a:a + step].contiguous(), torch.full((U,), a, dtype=torch.int32, device=DEV))
+    for x, y in zip(whole.tensors, parts.tensors):
+        assert torch.equal(x, y)
+    k, v = torch.empty_like(K), torch.empty_like(V)
+    whole.dynakv_packed_read(None, k, v)
+    for a in range(0, n, step):
+        at = torch.arange(a, min(n, a + step), dtype=torch.int32, device=DEV).expand(U, -1).contiguous()
+        k1, v1 = (torch.empty(U, at.shape[1], D, dtype=K.dtype, device=DEV) for _ in range(2))
+        whole.dynakv_packed_read(at, k1, v1)
+        assert torch.equal(k[:, a:a + step], k1) and torch.equal(v[:, a:a + step], v1)
+
+
 # ------------------------------------------------------------------------------------------- attention of drafted tokens
 def _plain_tree(Q, K, V, K1, V1, seen, scale):
     """One unit in float64: Q [T, G, D], K, V [L, D], K1, V1 [T, D], seen bool [T, T].  Returns out, lse and the quantities that
