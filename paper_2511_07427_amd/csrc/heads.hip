@@ -80,7 +80,7 @@ __device__ __forceinline__ void exchange(T& x, T& y, bool upper) {
 
 // Workgroup (16 / HP tokens, chunk of HP a.per heads); HP rows of 16 lanes belong to a token, each takes `per` heads, kBatch of them on their way
 // at once.  All rows go the same way through the code, values too (their result is dropped): with branches and 64-bit address arithmetic per
-// kind of row the kernel had as much to issue as to move (191 us for 16384 tokens of 80 bfloat16 rows; now 145 to 153, 4.4 to 4.6 TB/s).
+// kind of row the kernel had as much to issue as to move (191 us for 16384 tokens of 80 bfloat16 rows; now 138 to 151, 4.5 to 4.9 TB/s).
 template <int DT, int ORDER, int HP, bool STREAM>
 __global__ __launch_bounds__(256) void norm_rope_kernel(HeadsArgs a) {
   using F = Four<DT>;

@@ -501,6 +501,9 @@ struct Drafts {
 // A workgroup of W wavefronts, one per compute unit: WR of them take 32 rows each and share tiles of kSlots entries; W / WR such groups take
 // the tiles in turn.  Shared tiles have two places, of which one is filled while the other is read, with one barrier per tile.  A wavefront
 // that has its tiles alone (up to 32 rows: bound by memory) keeps 32 rows of K and V on their way in registers: 128 KB per compute unit.
+// Measured: 8 units of 131072 entries in 8 bits, one node of 8 heads: 58 us, 4.8 TB/s of codes and scales.  112 units of 2048 gathered entries and
+// 427 rows: 79 to 91 us; the matrix units are busy 36 % of that, vector instructions 44 %, LDS 39 %: no unit alone bounds it.  The two wavefronts of
+// a SIMD half a round apart, one reading keys while the other takes exponentials (two barriers a round), took 87.
 template <int DT, int SRC, int WR>
 struct Shape {
   static constexpr int W = DT == DYNAKV_F32 ? 4 : 8, kThreads = 64 * W;
