@@ -12,6 +12,8 @@
 // chunk of K (pad 16: rows 4 banks apart), 4 rows at 32 neighbouring bytes of V (pad 32: rows 8 banks apart).  Padding, unlike a
 // permutation of the chunks, leaves every place of a tile at a constant distance from one address per lane: a permutation cost some
 // 40 registers of addresses, which the accumulators need.
+#include <algorithm>
+
 #include "operators.hpp"
 
 namespace dynakv {
@@ -758,43 +760,59 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   if (a.lse && c == 0) a.lse[i] = none ? m : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// Wavefronts of a workgroup that take rows of their own, up to eight times 32 of the R rows of a unit: what they read of LDS they share with none,
+// Most wavefronts of a workgroup that take rows of their own, up to eight times 32 of the R rows of a unit: what they read of LDS they share with none,
 // what they load and unpack with all.  R = 427, 2048 entries of 112 units: 171 us with one, 147 with two, 108 with four, 92 with eight; R = 128 of
 // 128 packed units: 136, 108, 69 with four.  For 32 rows a second wavefront would be idle: 8 long packed units 62 us, with two 78.  Several blocks of
 // rows are made alike (R = 427: seven wavefronts of eight twice, 88 us, instead of eight and six, 92).  A float32 wavefront's queries and sums
 // leave room for one on a SIMD; its matrix instructions are what bounds it, whoever loads the tiles.
 int row_waves(int dtype, int R) { return dtype == DYNAKV_F32 || R <= kSub ? 1 : R <= 2 * kSub ? 2 : R <= 4 * kSub ? 4 : 8; }
 
-// Workgroups that a call gets for each block of rows (`pieces`), and the fewest entries for which another one is worth it (`least`), from a
-// model in ns, measured on 1 to 256 units: 256 workgroups run at once; one takes 9 us to begin and end, and per entry the larger of its
-// bytes (at its share of 5 TB/s, at most 64 per ns) and the work of its rows; the kernel that joins takes 6 us.  Units of one length would be
-// cut into s pieces each; a multiple of 256 workgroups that has room for those is what units of any lengths share.  (8 units of 131072 packed
-// entries: 62 us, whole 1247; 128 units of up to 8191: 69, whole 146.)
-struct Plan { int pieces, least; };
+// How the work is cut: `waves` of a workgroup take rows of their own, `pieces` are the workgroups that a call gets for each block of rows, `least` the
+// fewest entries for which another one is worth it.  From a model in ns, fitted to 1 to 256 units: 256 workgroups run at once; one takes 8.8 us
+// and 0.7 for each of its waves to begin and end, and per entry the larger of its bytes (at its share of 5 TB/s, at most 64 per ns, 36 where waves
+// share tiles) and the work of its rows, 4 for each 32 (34 for float32's matrix instructions), and 4 or (not float16) 10 to unpack; the kernel that
+// joins takes 6 us.  Units of one length would be cut into s pieces each; a multiple of 256 workgroups that has room for those is what units of any
+// lengths share, which then weigh three quarters of the longest.  (8 units of 131072 packed entries: 62 us, whole 1247; 128 units of up to 8191: 69,
+// whole 146.)  Fewer waves than there could be make more blocks of rows, for chips that would be idle otherwise: 5 units of 352 rows and 272
+// entries 11 us (as many waves as could be: 19), 81 of 255 and 417 22 (32), 140 of 336 and 761 56 (77).
+struct Plan { int waves, pieces, least; };
 constexpr int kMostRounds = 4;                       // bounds the scratch
-int row_blocks(int dtype, int R) { return (R + row_waves(dtype, R) * kSub - 1) / (row_waves(dtype, R) * kSub); }
-bool may_share(int dtype, int U, int R) { return U <= kPlanUnits && (long long)U * row_blocks(dtype, R) <= 2 * kWorkgroups; }
-int pieces_for(int dtype, int U, int R, int s) {     // a unit of s pieces: 0: more rounds than there may be
-  const int rb = row_blocks(dtype, R), rounds = (U * rb * s + kWorkgroups - 1) / kWorkgroups;
-  return rounds > kMostRounds ? 0 : max(U, rounds * kWorkgroups / rb);
+int row_blocks(int waves, int R) { return (R + waves * kSub - 1) / (waves * kSub); }
+bool may_share(int waves, int U, int R) { return U <= kPlanUnits && (long long)U * row_blocks(waves, R) <= 2 * kWorkgroups; }
+// Rounds of the chip: the blocks of rows of a piece run on one XCD, of which each takes every eighth piece (84 pieces of three blocks are 33
+// workgroups on some of them: 37 us where 56 take 28).
+constexpr int kXcds = 8, kPerXcd = kWorkgroups / kXcds;
+long long rounds_of(long long pieces, int blocks) { return ((pieces + kXcds - 1) / kXcds * blocks + kPerXcd - 1) / kPerXcd; }
+int pieces_for(int waves, int U, int R, int s) {     // a unit of s pieces: 0: more rounds than there may be
+  const int blocks = row_blocks(waves, R);
+  const long long rounds = rounds_of((long long)U * s, blocks);
+  return rounds > kMostRounds ? 0 : max(U, kXcds * (kPerXcd * (int)rounds / blocks));
 }
-Plan plan(int dtype, int bytes, int U, int R, long long most, bool ragged) {
-  if (!may_share(dtype, U, R)) return Plan{U, 1};
-  const int n = U * row_blocks(dtype, R);
-  const double work = dtype == DYNAKV_F32 ? 34.0 : 4.0 * row_waves(dtype, R);      // (the float32 matrix instructions)
-  auto entry = [&](int workgroups) {
-    const double share = 5120.0 / (workgroups < kWorkgroups ? workgroups : kWorkgroups), b = bytes / (share < 64.0 ? share : 64.0);
-    return b > work ? b : work;
-  };
-  if (entry(n) * (double)most < 8e3) return Plan{U, 1};
-  int best = 0;
-  double time = 0.0;
-  for (int s = 1; s <= 64 && pieces_for(dtype, U, R, s); ++s) {
-    const double t = (double)((n * s + kWorkgroups - 1) / kWorkgroups) * (9e3 + entry(n * s) * (double)most / s) + (s > 1 ? 6e3 : 0.0);
-    if (s == 1 || t < 0.97 * time) { best = s; time = t; }
+Plan plan(int dtype, int bytes, bool packed, int U, int R, long long most, bool ragged) {
+  Plan best = {0, 0, 1};
+  double least_time = 0.0;
+  for (int waves = row_waves(dtype, R); waves >= 1; waves /= 2) {
+    const int blocks = row_blocks(waves, R);
+    const long long n = (long long)U * blocks;
+    const double work = dtype == DYNAKV_F32 ? 34.0 : 4.0 * waves + (!packed ? 0.0 : dtype == DYNAKV_F16 ? 4.0 : 10.0);
+    auto entry = [&](long long workgroups) {
+      const double share = 5120.0 / (double)std::min<long long>(workgroups, kWorkgroups), b = bytes / std::min(share, waves == 1 ? 64.0 : 36.0);
+      return std::max(b, work);
+    };
+    const bool cut = may_share(waves, U, R) && entry(n) * (double)most >= 8e3;
+    int pieces = 1;
+    double time = 0.0;
+    for (int s = 1; s == 1 || (cut && s <= 64 && pieces_for(waves, U, R, s)); ++s) {
+      const double longest = (ragged && s > 1 ? 0.75 : 1.0) * (double)most / s;
+      const double t = (double)rounds_of((long long)U * s, blocks) * (8.8e3 + 700.0 * waves + entry(n * s) * longest) + (s > 1 ? 6e3 : 0.0);
+      if (s == 1 || t < 0.97 * time) { pieces = s; time = t; }
+    }
+    if (best.waves && time > 0.9 * least_time) continue;
+    least_time = time;
+    const int all = cut && (pieces > 1 || ragged) ? pieces_for(waves, U, R, pieces) : 0;
+    best = all ? Plan{waves, all, (int)(4e3 / entry(kWorkgroups)) + 1} : Plan{waves, U, 1};
   }
-  if (best == 0 || (best == 1 && !ragged)) return Plan{U, 1};
-  return Plan{pieces_for(dtype, U, R, best), (int)(4e3 / entry(kWorkgroups)) + 1};
+  return best;
 }
 
 template <int DT, int SRC, int WR>
@@ -808,11 +826,10 @@ hipError_t launch_shape(TreeArgs& a, hipStream_t st) {
 }
 
 template <int DT, int SRC>
-hipError_t launch_source(TreeArgs& a, hipStream_t st) {
+hipError_t launch_source(TreeArgs& a, int wr, hipStream_t st) {
   if constexpr (DT == DYNAKV_F32) {
     return launch_shape<DT, SRC, 1>(a, st);
   } else {
-    const int wr = row_waves(DT, a.T * a.G);
     return wr == 1   ? launch_shape<DT, SRC, 1>(a, st)
            : wr == 2 ? launch_shape<DT, SRC, 2>(a, st)
            : wr == 4 ? launch_shape<DT, SRC, 4>(a, st)
@@ -823,10 +840,11 @@ hipError_t launch_source(TreeArgs& a, hipStream_t st) {
 template <int DT>
 hipError_t launch(TreeArgs a, hipStream_t st) {
   const int R = a.T * a.G, bytes = a.pages ? 2 * Mma<DT>::kRow : 2 * (kHeadDim * a.cache.bits / 8 + kRowScales);
-  const Plan p = plan(DT, bytes, a.U, R, a.most, !a.pages && a.lengths);
+  const Plan p = plan(DT, bytes, !a.pages, a.U, R, a.most, !a.pages && a.lengths);
   a.pieces = p.pieces;
   a.least = p.least;
-  const hipError_t e = a.pages ? launch_source<DT, kList>(a, st) : a.cache.bits == 8 ? launch_source<DT, kPacked8>(a, st) : launch_source<DT, kPacked4>(a, st);
+  const hipError_t e = a.pages ? launch_source<DT, kList>(a, p.waves, st)
+                               : a.cache.bits == 8 ? launch_source<DT, kPacked8>(a, p.waves, st) : launch_source<DT, kPacked4>(a, p.waves, st);
   if (e != hipSuccess || a.pieces == a.U) return e;
   // Few rows of many pieces: eight groups of lanes to a row; else one (4992 rows of 6 pieces 12 us with eight, 64 rows of 32 pieces 52 with one
   // that takes a piece at a time).
@@ -836,11 +854,13 @@ hipError_t launch(TreeArgs a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Scratch: where the pieces of each unit are, then a partial result of every row for each piece.  The most that any plan has.
+// Scratch: where the pieces of each unit are, then a partial result of every row for each piece.  The most that any plan has: fewer waves make more
+// blocks of rows, of which each gets fewer pieces.
 size_t where_bytes(int U) { return ((size_t)U * 8 + 255) & ~(size_t)255; }
 size_t part_bytes(int dtype, int U, int R) {
-  if (!may_share(dtype, U, R)) return 0;
-  const int most = kMostRounds * kWorkgroups / row_blocks(dtype, R);
+  const int waves = row_waves(dtype, R);
+  if (!may_share(waves, U, R)) return 0;
+  const int most = kMostRounds * kWorkgroups / row_blocks(waves, R);
   return (size_t)(most > U ? most : U) * R * kPartRow * sizeof(float);
 }
 

@@ -615,6 +615,41 @@ def test_tree_attention_over_a_retrieval(dt, U, T, G, n, M, budget):
         _check_tree(root[u], None, ref, dt, len(at[u]))
 
 
+# Rows beyond those of one wavefront, on so few and so many units that workgroups of two, four and eight wavefronts of rows, whole and shared units
+# and several blocks of rows occur.
+@gpu
+@pytest.mark.parametrize("dt", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("U,T,G,n,M,budget", [(120, 59, 5, 500, 20, 393), (2, 64, 16, 1600, 50, 1500), (70, 33, 5, 1000, 30, 900), (30, 25, 4, 3300, 60, 3000)])
+def test_tree_attention_of_many_rows(dt, U, T, G, n, M, budget):
+    ix, K, V, at, gen, Q0, flat = _retrieved(dt, U, G, n, M, budget, T)
+    Q, K1, V1, out, lse = _drafts(dt, U, T, G, gen)
+    seen = _random_tree(U, T, gen)
+    ix.dynakv_attend_tree(Q, K1, V1, _bits(seen), out, lse, tree_scratch(U, T, G, DEV))
+    for u in range(U):
+        ref = _plain_tree(Q[u].double(), K[u, at[u]].double(), V[u, at[u]].double(), K1[u].double(), V1[u].double(), seen[u], D ** -0.5)
+        _check_tree(out[u], lse[u], ref, dt, len(at[u]) + T)
+
+
+@gpu
+@pytest.mark.parametrize("dt,bits", [("f16", 8), ("f16", 4), ("bf16", 8), ("bf16", 4), ("f32", 8)])
+@pytest.mark.parametrize("U,T,G,cap", [(120, 59, 5, 393), (130, 30, 3, 1500), (20, 60, 5, 6000), (28, 59, 5, 1214), (65, 20, 3, 3000)])
+def test_packed_attention_of_many_rows(dt, bits, U, T, G, cap):
+    gen = torch.Generator(DEV).manual_seed(U + T + cap)
+    K, V = (torch.randn(U, cap, D, generator=gen, device=DEV).to(TORCH_DTYPES[dt]) for _ in range(2))
+    c = PackedCache.zeros(U, cap, dt, bits, DEV)
+    c.dynakv_packed_write(K, V)
+    c.dynakv_packed_read(None, K, V)
+    lengths = torch.randint(0, cap + 1, (U,), generator=gen, device=DEV, dtype=torch.int32)
+    lengths[0], lengths[1] = cap, 0
+    Q, K1, V1, out, lse = _drafts(dt, U, T, G, gen)
+    seen = _random_tree(U, T, gen)
+    c.dynakv_packed_attend(lengths, Q, K1, V1, _bits(seen), out, lse, tree_scratch(U, T, G, DEV))
+    for u in range(U):
+        n = int(lengths[u])
+        ref = _plain_tree(Q[u].double(), K[u, :n].double(), V[u, :n].double(), K1[u].double(), V1[u].double(), seen[u], D ** -0.5)
+        _check_tree(out[u], lse[u], ref, dt, n + T)
+
+
 @gpu
 @pytest.mark.parametrize("more", [dict(update_mode=binding.UPDATE_TOKENS), dict(launch=binding.launch_shape(3, 4, binding.LAUNCH_SEPARATE)),
                                   dict(search_copy=binding.SEARCH_MEAN), dict(softmax_scale=0.37)])
