@@ -619,7 +619,8 @@ def test_tree_attention_over_a_retrieval(dt, U, T, G, n, M, budget):
 # and several blocks of rows occur.
 @gpu
 @pytest.mark.parametrize("dt", ["f16", "bf16", "f32"])
-@pytest.mark.parametrize("U,T,G,n,M,budget", [(120, 59, 5, 500, 20, 393), (2, 64, 16, 1600, 50, 1500), (70, 33, 5, 1000, 30, 900), (30, 25, 4, 3300, 60, 3000)])
+@pytest.mark.parametrize("U,T,G,n,M,budget", [(120, 59, 5, 500, 20, 393), (2, 64, 16, 1600, 50, 1500), (70, 33, 5, 1000, 30, 900), (30, 25, 4, 3300, 60, 3000),
+                                              (27, 11, 5, 1500, 40, 1266), (110, 10, 5, 700, 20, 600)])
 def test_tree_attention_of_many_rows(dt, U, T, G, n, M, budget):
     ix, K, V, at, gen, Q0, flat = _retrieved(dt, U, G, n, M, budget, T)
     Q, K1, V1, out, lse = _drafts(dt, U, T, G, gen)
