@@ -364,6 +364,7 @@ size_t dynakv_tree_scratch_bytes(int32_t n_units, int32_t n_nodes, int32_t group
  *                   infinities included, has no part in its output
  *   out             device, [U][n_nodes][G][head_dim] in cfg.dtype; zeros where a node sees nothing
  *   lse             device, float32 [U][n_nodes][G] or null: log-sum-exp of the scaled logits (-inf where it sees nothing)
+ *                   A NaN among the logits that a row sees (of a query, of a key) makes its out and lse NaN
  *   scratch         device, 16-byte aligned, at least dynakv_tree_scratch_bytes(U, n_nodes, G) (else DYNAKV_ECAPACITY);
  *                   contents need no initialisation
  * Products and sums are float32; with 16-bit storage a probability is rounded to that type before it weights a value. */

@@ -172,6 +172,9 @@ struct Rows {
   float m, l;                                        // what the weights are relative to (log2), and their sum over the lane's half of the entries
   f16v o[4];
 };
+// Whether a part of a row's entries (a wavefront's, a piece's) has none that the row sees: its sum is 0 then.  The maximum alone does not say so: it
+// passes over scores that are NaN, whose sum is NaN and has to come out.
+__device__ __forceinline__ bool saw_nothing(float m, float l) { return m == -__builtin_inff() && l == 0.f; }
 
 // What the scores of 32 slots begin with: 0, or -inf where a slot holds nothing.  (Conditions per slot on the finished scores, the same
 // for every row, took as many instructions as the exponentials.)
@@ -684,15 +687,15 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
     f4 o = {0, 0, 0, 0};
 #pragma unroll
     for (int w = 0; w < kGroups; ++w) {
-      if (mw[w] == -__builtin_inff()) continue;       // that wavefront saw nothing of this row
-      const float f = mw[w] == m ? 1.f : __builtin_amdgcn_exp2f(mw[w] - m);
       const float* x = mo + (w * WR * kSub + r) * kOut;
+      if (saw_nothing(mw[w], x[kHeadDim + 1])) continue;
+      const float f = mw[w] == m ? 1.f : __builtin_amdgcn_exp2f(mw[w] - m);
       l += f * x[kHeadDim + 1];
       o += f * *(const f4*)(x + c);
     }
     const size_t to = (size_t)u * R + rr;
     if (ns == 1) {
-      const bool none = m == -__builtin_inff();
+      const bool none = saw_nothing(m, l);
       M::store4(a.out, to * kHeadDim + c, none ? f4{0, 0, 0, 0} : o / l);
       if (a.lse && c == 0) a.lse[to] = none ? m : (m + __builtin_amdgcn_logf(l)) * kLn2;
     } else {
@@ -718,7 +721,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   float ms[8], ls[8], m = -__builtin_inff(), l = 0.f;
   f4 os[8], o = {0, 0, 0, 0};
   auto add = [&](float mk, float lk, const f4& ok) {
-    if (mk == -__builtin_inff()) return;             // saw nothing of this row, whatever its sums hold
+    if (saw_nothing(mk, lk)) return;
     const float f = mk == m ? 1.f : __builtin_amdgcn_exp2f(mk - m);
     l += f * lk;
     o += f * ok;
@@ -729,13 +732,12 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
       const int s = s0 + P * k;
       const float* x = p + (size_t)min(s, ns - 1) * R * kPartRow;
       ms[k] = s < ns ? x[kHeadDim] : -__builtin_inff();
-      ls[k] = x[kHeadDim + 1];
+      ls[k] = s < ns ? x[kHeadDim + 1] : 0.f;
       os[k] = *(const f4*)(x + c);
     }
     float top = m;
 #pragma unroll
     for (int k = 0; k < 8; ++k) top = fmaxf(top, ms[k]);
-    if (top == -__builtin_inff()) continue;
     const float f = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
     m = top;
     l *= f;
@@ -755,7 +757,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) add(sm[k][kHeadDim], sm[k][kHeadDim + 1], *(const f4*)&sm[k][c]);
   }
-  const bool none = m == -__builtin_inff();
+  const bool none = saw_nothing(m, l);
   Mma<DT>::store4(a.out, i * kHeadDim + c, none ? f4{0, 0, 0, 0} : o / l);
   if (a.lse && c == 0) a.lse[i] = none ? m : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }

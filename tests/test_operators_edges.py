@@ -1,0 +1,112 @@
+"""Attention of drafted tokens where something that a row sees is NaN.
+
+Bounds are those of test_operators.py unless derived here."""
+import os
+import sys
+
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+
+from paper_2511_07427_amd.binding import TORCH_DTYPES, PackedCache, tree_scratch  # noqa: E402
+from test_operators import D, DEV, _bits, _check_tree, _drafts, _plain_tree, _random_tree, _retrieved  # noqa: E402
+
+gpu = pytest.mark.gpu
+
+
+def _filled(dt, bits, U, cap, gen, spoil=None):
+    """A packed cache of `cap` random entries a unit, and the values that it holds; spoil(K, V) changes them before they are written."""
+    K, V = (torch.randn(U, max(1, cap), D, generator=gen, device=DEV).to(TORCH_DTYPES[dt]) for _ in range(2))
+    if spoil:
+        spoil(K, V)
+    c = PackedCache.zeros(U, max(1, cap), dt, bits, DEV)
+    c.dynakv_packed_write(K, V)
+    c.dynakv_packed_read(None, K, V)
+    return c, K[:, :cap], V[:, :cap]
+
+
+def _check_with_nan(got, got_lse, ref, dt, L):
+    """Rows whose definition is NaN are NaN throughout, the others right.  Returns how many are."""
+    gone = ref[1].isnan()
+    assert got[gone].isnan().all() and got_lse[gone].isnan().all()
+    got, got_lse, ref = got.clone(), got_lse.clone(), [x.clone() for x in ref]
+    for x in (got, got_lse, *ref):
+        x[gone] = 0
+    _check_tree(got, got_lse, ref, dt, L)
+    return int(gone.sum())
+
+
+def _chain(T):
+    return torch.ones(T, T, dtype=torch.bool, device=DEV).tril()
+
+
+# Calls whose rows are one group's, several groups' of a workgroup, several workgroups', and joined from few and from many pieces.
+SHAPES = [(2, 1, 1, 0), (2, 1, 4, 33), (2, 5, 3, 700), (1, 9, 4, 6000), (1, 1, 2, 60000), (3, 40, 8, 900), (600, 1, 2, 70)]
+
+
+@gpu
+@pytest.mark.parametrize("dt,bits", [("f16", 8), ("bf16", 4), ("f32", 8)])
+@pytest.mark.parametrize("U,T,G,cap", SHAPES)
+def test_a_query_that_is_nan_gives_nan(dt, bits, U, T, G, cap):
+    gen = torch.Generator(DEV).manual_seed(U + T + cap)
+    c, K, V = _filled(dt, bits, U, cap, gen)
+    Q, K1, V1, out, lse = _drafts(dt, U, T, G, gen)
+    Q[0, T - 1, G - 1, 3] = float("nan")
+    c.dynakv_packed_attend(torch.full((U,), cap, dtype=torch.int32, device=DEV), Q, K1, V1, None, out, lse, tree_scratch(U, T, G, DEV))
+    for u in range(min(U, 3)):
+        ref = _plain_tree(Q[u].double(), K[u].double(), V[u].double(), K1[u].double(), V1[u].double(), _chain(T), D ** -0.5)
+        assert _check_with_nan(out[u], lse[u], ref, dt, cap + T) == (1 if u == 0 else 0)
+
+
+@gpu
+@pytest.mark.parametrize("dt,bits", [("f16", 4), ("bf16", 8), ("f32", 8)])
+@pytest.mark.parametrize("T,G", [(1, 1), (3, 4), (30, 4)])
+@pytest.mark.parametrize("cap,first,last", [(1, 0, 1), (33, 32, 33), (65, 64, 65), (65, 63, 64), (5000, 4999, 5000), (20000, 3000, 9000), (700, 0, 700)])
+def test_keys_that_are_nan_reach_every_row(dt, bits, T, G, cap, first, last):
+    # (one entry by itself in a tile, one at a tile's end, whole pieces, everything)
+    gen = torch.Generator(DEV).manual_seed(cap + T)
+    U = 2
+
+    def spoil(K, V):
+        K[0, first:last, 70] = float("nan")
+    c, K, V = _filled(dt, bits, U, cap, gen, spoil)
+    Q, K1, V1, out, lse = _drafts(dt, U, T, G, gen)
+    c.dynakv_packed_attend(None, Q, K1, V1, None, out, lse, tree_scratch(U, T, G, DEV))
+    assert out[0].isnan().all() and lse[0].isnan().all()
+    ref = _plain_tree(Q[1].double(), K[1].double(), V[1].double(), K1[1].double(), V1[1].double(), _chain(T), D ** -0.5)
+    _check_tree(out[1], lse[1], ref, dt, cap + T)
+
+
+@gpu
+@pytest.mark.parametrize("dt,bits", [("f16", 8), ("bf16", 4), ("f32", 8)])
+@pytest.mark.parametrize("U,T,G,cap", SHAPES)
+def test_drafted_keys_that_are_nan_reach_the_rows_that_see_them(dt, bits, U, T, G, cap):
+    gen = torch.Generator(DEV).manual_seed(U + T + cap)
+    c, K, V = _filled(dt, bits, U, cap, gen)
+    Q, K1, V1, out, lse = _drafts(dt, U, T, G, gen)
+    K1[0, T - 1] = float("nan")
+    seen = _random_tree(U, T, gen)
+    seen[0, :, T - 1] = False
+    seen[0, T - 1, T - 1] = True                                 # the last node sees itself, no other does
+    if T > 1:
+        seen[0, 0] = False
+    c.dynakv_packed_attend(torch.full((U,), cap, dtype=torch.int32, device=DEV), Q, K1, V1, _bits(seen), out, lse, tree_scratch(U, T, G, DEV))
+    for u in range(min(U, 3)):
+        ref = _plain_tree(Q[u].double(), K[u].double(), V[u].double(), K1[u].double(), V1[u].double(), seen[u], D ** -0.5)
+        assert _check_with_nan(out[u], lse[u], ref, dt, cap + T) == (G if u == 0 else 0)
+
+
+@gpu
+@pytest.mark.parametrize("dt", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("U,T,G,budget", [(1, 1, 4, 20), (2, 6, 3, 300), (1, 40, 4, 900)])
+def test_nan_over_a_retrieval(dt, U, T, G, budget):
+    ix, K, V, at, gen, _, _ = _retrieved(dt, U, G, 1000, 100, budget, T)
+    Q, K1, V1, out, lse = _drafts(dt, U, T, G, gen)
+    Q[0, 0, 0, 5] = float("nan")
+    K1[U - 1, T - 1, 9] = float("nan")
+    ix.dynakv_attend_tree(Q, K1, V1, None, out, lse, tree_scratch(U, T, G, DEV))
+    for u in range(U):
+        ref = _plain_tree(Q[u].double(), K[u, at[u]].double(), V[u, at[u]].double(), K1[u].double(), V1[u].double(), _chain(T), D ** -0.5)
+        gone = _check_with_nan(out[u], lse[u], ref, dt, len(at[u]) + T)
+        assert gone == (G if u == U - 1 else 0) + (1 if u == 0 else 0) - (1 if u == 0 == U - 1 and T == 1 else 0)
