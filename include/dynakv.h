@@ -356,7 +356,9 @@ size_t dynakv_tree_scratch_bytes(int32_t n_units, int32_t n_nodes, int32_t group
 /* Attention of a tree of drafted tokens (one token: plain decoding; a chain: a chunk of a prompt) over the entries that the
  * last retrieval of the index gathered, one softmax over those and the drafted tokens each node sees:
  *   out[u][i][g] = softmax(scale * q . {gathered keys, K_tree[u][j] for the bits j of tree[u][i]}) . {values}
- * The index must not have changed since that retrieval (DYNAKV_ESTATE; a captured graph holds both calls), and does not change.
+ * The index must not have changed since that retrieval (else DYNAKV_ESTATE), and does not change.  A captured graph holds both calls or
+ * neither: in a graph the retrieval is one of the same capture, outside it is one that was not captured (else DYNAKV_ESTATE).  The handle
+ * sees calls, not replays: after the replay of a graph that retrieves or changes the index, a retrieval comes first.
  *   Q               device, [U][n_nodes][G][head_dim] in cfg.dtype, 1 <= n_nodes <= 64; U < 2^22, U * n_nodes * G < 2^28
  *   K_tree, V_tree  device, [U][n_nodes][head_dim] in cfg.dtype, or both null: the gathered entries alone
  *   tree            device, uint64 [U][n_nodes]: bit j: node i sees drafted token j (itself included where its bit is set; bits

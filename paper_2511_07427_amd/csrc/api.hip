@@ -19,6 +19,7 @@ struct dynakv_index {
   bool built;
   int local_count;   // local update: appends enqueued since the last local clustering
   bool listed;       // the gather list is that of a retrieval since which the index has not changed
+  unsigned long long list_capture;   // the stream capture that this retrieval was recorded in (it has not run then); 0: none
   int list_budget;   // its token budget
   // optional timing of the gather + attention kernel
   bool profiling;
@@ -186,6 +187,7 @@ dynakv_status_t dynakv_create(const dynakv_config_t* cfg, void* workspace, size_
   ix->built = false;
   ix->local_count = 0;
   ix->listed = false;
+  ix->list_capture = 0;
   ix->list_budget = 0;
   ix->profiling = false;
   ix->n_prof = 0;
@@ -213,6 +215,18 @@ dynakv_status_t dynakv_build_index(dynakv_index_t* ix, const void* K, const void
   return DYNAKV_OK;
 }
 
+// The capture that work enqueued on `st` is recorded in, 0 where it runs.  (The default stream cannot be captured; asked about it during
+// a capture elsewhere the runtime reports an error, which must not be the next launch's.)
+static unsigned long long capture_of(hipStream_t st) {
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  unsigned long long id = 0;
+  if (hipStreamGetCaptureInfo(st, &status, &id) != hipSuccess) {
+    (void)hipGetLastError();
+    return 0;
+  }
+  return status == hipStreamCaptureStatusNone ? 0 : id;
+}
+
 // Retrieval on the index as `view` shows it (the index's own view, or one whose scratch arrays point elsewhere),
 // and with kin != null the append as well if one kernel can do both (*appended says whether it did), and with
 // `split` the due splits too (*appended then covers them).
@@ -238,6 +252,7 @@ static dynakv_status_t retrieve_impl(dynakv_index_t* ix, const View& view, const
     }
   }
   ix->listed = !*appended;
+  ix->list_capture = capture_of(st);
   ix->list_budget = token_budget;
   return DYNAKV_OK;
 }
@@ -466,7 +481,7 @@ dynakv_status_t dynakv_attend_tree(dynakv_index_t* ix, const void* Q, int32_t n_
   TreeArgs a = {};
   const dynakv_status_t rc = tree_args(&a, v.U, n_nodes, v.G, v.dtype, v.scale_f, Q, K_tree, V_tree, tree, out, lse, scratch, scratch_bytes);
   if (rc != DYNAKV_OK) return rc;
-  if (!ix->built || !ix->listed) return DYNAKV_ESTATE;
+  if (!ix->built || !ix->listed || ix->list_capture != capture_of((hipStream_t)stream)) return DYNAKV_ESTATE;
   a.pages = v.pages; a.unit_pages = (size_t)v.Pcap * kPageElems * elem_size(v.dtype);
   a.plist = v.plist; a.n_list = v.n_list; a.Lcap = v.Lcap;
   a.most = std::min(ix->list_budget, v.Ncap);

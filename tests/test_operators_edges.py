@@ -110,3 +110,51 @@ def test_nan_over_a_retrieval(dt, U, T, G, budget):
         ref = _plain_tree(Q[u].double(), K[u, at[u]].double(), V[u, at[u]].double(), K1[u].double(), V1[u].double(), _chain(T), D ** -0.5)
         gone = _check_with_nan(out[u], lse[u], ref, dt, len(at[u]) + T)
         assert gone == (G if u == U - 1 else 0) + (1 if u == 0 else 0) - (1 if u == 0 == U - 1 and T == 1 else 0)
+
+
+@gpu
+def test_a_retrieval_that_is_only_captured_lists_nothing_outside_its_graph():
+    """Capturing a retrieval does not run it: attention over its list belongs into the same graph, and a graph's attention needs its own retrieval."""
+    U, T, G, budget = 2, 3, 4, 100
+    ix, K, V, at, gen, Q0, flat = _retrieved("f16", U, G, 300, 20, budget, 4)
+    Q, K1, V1, out, lse = _drafts("f16", U, T, G, gen)
+    scratch, side, other = tree_scratch(U, T, G, DEV), torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def retrieve():
+        ix.dynakv_retrieve_attend(Q0, budget, flat, None)
+
+    def attend():
+        ix.dynakv_attend_tree(Q, K1, V1, None, out, lse, scratch)
+
+    def refused():
+        out.fill_(3.0)
+        with pytest.raises(RuntimeError, match="out of order"):
+            attend()
+        assert torch.cuda.is_current_stream_capturing() or bool((out == 3.0).all())
+    # (the list of the eager retrieval before is there throughout: no call reads what was never written)
+    before, alone, later, both = (torch.cuda.CUDAGraph() for _ in range(4))
+    with torch.cuda.graph(before, stream=side):
+        refused()                                                # the list is not this graph's
+    attend()                                                     # nothing has changed for eager calls
+    with torch.cuda.graph(alone, stream=side):
+        retrieve()
+    refused()                                                    # the retrieval has not run
+    with torch.cuda.graph(later, stream=side):
+        refused()                                                # it is another graph's
+    with torch.cuda.graph(both, stream=side):
+        retrieve()
+        other.wait_stream(side)
+        with torch.cuda.stream(other):
+            attend()                                             # on a stream that joins the capture
+        side.wait_stream(other)
+    refused()
+    for i in range(4):
+        Q0.copy_(torch.randn(Q0.shape, generator=gen, device=DEV))
+        out.fill_(9.0)
+        both.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        retrieve()
+        attend()
+        assert torch.equal(out, got), i
