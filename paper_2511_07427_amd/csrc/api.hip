@@ -399,8 +399,9 @@ dynakv_status_t dynakv_import_state(dynakv_index_t* ix, const dynakv_state_t* sr
 
 // ---- operators beside the index ----------------------------------------------------------------------
 static bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
-// A grid has fewer than 2^32 work-items: what keeps each of these kernels below that.  Norm + rotation: at most 64 / 3 work-items for a row
-// (few heads to a token); packed rows: 16 each; attention: 512 for every unit and every further 256 rows (float32: 256, 32 rows).
+// A grid has fewer than 2^32 work-items: what keeps each of these kernels below that.  Norm + rotation: of many tokens at most 64 / 3 work-items
+// for a row (few heads to a token), of few 2^19 in all; packed rows: 16 each; attention: 512 for every unit and every further 256 rows (float32:
+// 256, 32 rows), or where more blocks of rows are made 512 for each of at most 2^22 (kMostBlocks).
 constexpr unsigned kMaxHeadRows = 1u << 27;
 constexpr long long kMaxPackedRows = 1ll << 28, kMaxTreeRows = 1ll << 28;
 constexpr int kMaxTreeUnits = 1 << 22;

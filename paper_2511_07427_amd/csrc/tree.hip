@@ -779,6 +779,9 @@ int row_waves(int dtype, int R) { return dtype == DYNAKV_F32 || R <= kSub ? 1 : 
 // entries 11 us (as many waves as could be: 19), 81 of 255 and 417 22 (32), 140 of 336 and 761 56 (77).
 struct Plan { int waves, pieces, least; };
 constexpr int kMostRounds = 4;                       // bounds the scratch
+// Fewer waves than there could be make at most this many workgroups of 512: a launch has fewer than 2^32 work-items.  (As many as could be make a
+// workgroup per unit and every further 256 rows, which the limits of the call keep below that.)
+constexpr long long kMostBlocks = 1ll << 22;
 int row_blocks(int waves, int R) { return (R + waves * kSub - 1) / (waves * kSub); }
 bool may_share(int waves, int U, int R) { return U <= kPlanUnits && (long long)U * row_blocks(waves, R) <= 2 * kWorkgroups; }
 // Rounds of the chip: the blocks of rows of a piece run on one XCD, of which each takes every eighth piece (84 pieces of three blocks are 33
@@ -796,6 +799,7 @@ Plan plan(int dtype, int bytes, bool packed, int U, int R, long long most, bool 
   for (int waves = row_waves(dtype, R); waves >= 1; waves /= 2) {
     const int blocks = row_blocks(waves, R);
     const long long n = (long long)U * blocks;
+    if (best.waves && n > kMostBlocks) break;
     const double work = dtype == DYNAKV_F32 ? 34.0 : 4.0 * waves + (!packed ? 0.0 : dtype == DYNAKV_F16 ? 4.0 : 10.0);
     auto entry = [&](long long workgroups) {
       const double share = 5120.0 / (double)std::min<long long>(workgroups, kWorkgroups), b = bytes / std::min(share, waves == 1 ? 64.0 : 36.0);
