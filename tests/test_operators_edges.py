@@ -1,6 +1,5 @@
-"""Attention of drafted tokens where something that a row sees is NaN.
-
-Bounds are those of test_operators.py unless derived here."""
+"""Attention of drafted tokens where something that a row sees is NaN, in graphs that hold only a part of it, and in its plainest calls: a token that
+sees itself, a chain without bits, a denominator of 3e7 like terms.  Bounds are those of test_operators.py unless derived here."""
 import os
 import sys
 
@@ -10,7 +9,7 @@ import torch
 sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
 
 from paper_2511_07427_amd.binding import TORCH_DTYPES, PackedCache, tree_scratch  # noqa: E402
-from test_operators import D, DEV, _bits, _check_tree, _drafts, _plain_tree, _random_tree, _retrieved  # noqa: E402
+from test_operators import D, DEV, HALF, U32, _bits, _check_tree, _drafts, _plain_tree, _random_tree, _retrieved  # noqa: E402
 
 gpu = pytest.mark.gpu
 
@@ -158,3 +157,75 @@ def test_a_retrieval_that_is_only_captured_lists_nothing_outside_its_graph():
         retrieve()
         attend()
         assert torch.equal(out, got), i
+
+
+@gpu
+@pytest.mark.parametrize("dt,bits", [("f16", 8), ("f16", 4), ("bf16", 8), ("bf16", 4), ("f32", 8), ("f32", 4)])
+@pytest.mark.parametrize("U,T,G,cap", [(3, 1, 1, 1), (2, 1, 8, 64), (2, 1, 3, 4097), (600, 1, 2, 50), (2, 2, 4, 33), (3, 33, 3, 300), (1, 64, 16, 700)])
+def test_a_chain_without_bits(dt, bits, U, T, G, cap):
+    # node i sees drafted tokens 0..i; one token: decoding, it sees the cache and itself
+    gen = torch.Generator(DEV).manual_seed(U + T + cap)
+    c, K, V = _filled(dt, bits, U, cap, gen)
+    Q, K1, V1, out, lse = _drafts(dt, U, T, G, gen)
+    K1[:, T - 1] += Q[:, T - 1, 0]                               # a weight that counts
+    scratch = tree_scratch(U, T, G, DEV)
+    for lengths in (None, torch.zeros(U, dtype=torch.int32, device=DEV)):
+        c.dynakv_packed_attend(lengths, Q, K1, V1, None, out, lse, scratch)
+        n = cap if lengths is None else 0
+        for u in range(min(U, 3)):
+            ref = _plain_tree(Q[u].double(), K[u, :n].double(), V[u, :n].double(), K1[u].double(), V1[u].double(), _chain(T), D ** -0.5)
+            _check_tree(out[u], lse[u], ref, dt, n + T)
+        again, lse2 = torch.empty_like(out), torch.empty_like(lse)
+        c.dynakv_packed_attend(lengths, Q, K1, V1, _bits(_chain(T).expand(U, T, T)), again, lse2, scratch)
+        assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@gpu
+@pytest.mark.parametrize("dt", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("U,T,G,budget", [(2, 1, 4, 300), (1, 1, 7, 1), (3, 5, 2, 200)])
+def test_a_chain_without_bits_over_a_retrieval(dt, U, T, G, budget):
+    ix, K, V, at, gen, _, _ = _retrieved(dt, U, G, 900, 60, budget, T)
+    Q, K1, V1, out, lse = _drafts(dt, U, T, G, gen)
+    ix.dynakv_attend_tree(Q, K1, V1, None, out, lse, tree_scratch(U, T, G, DEV))
+    for u in range(U):
+        ref = _plain_tree(Q[u].double(), K[u, at[u]].double(), V[u, at[u]].double(), K1[u].double(), V1[u].double(), _chain(T), D ** -0.5)
+        _check_tree(out[u], lse[u], ref, dt, len(at[u]) + T)
+
+
+@gpu
+@pytest.mark.parametrize("dt", ["f16", "bf16", "f32"])
+def test_every_entry_beyond_32_bits_counts(dt):
+    """2^25 + 77 entries, 4.3 GB of codes, of which 50 are random and the others are alike: key 0, value 1 in column 7.  With a largest logit near 16 both
+    kinds have a share in the denominator, so an entry left out or taken twice for every few hundred shows."""
+    cap, G = (1 << 25) + 77, 2
+    gen = torch.Generator(DEV).manual_seed(3)
+    c = PackedCache.zeros(1, cap, dt, 8, DEV)
+    c.tensors[2][0, :, 7] = 1                                    # value codes and their block's scale, 2^0
+    c.tensors[3][0, :, 0] = 127
+    K, V = (torch.randn(1, 50, D, generator=gen, device=DEV).to(TORCH_DTYPES[dt]) for _ in range(2))
+    start = torch.tensor([cap - 50], dtype=torch.int32, device=DEV)
+    c.dynakv_packed_write(K, V, start)
+    k, v = torch.empty_like(K), torch.empty_like(V)
+    c.dynakv_packed_read((start[:, None] + torch.arange(50, device=DEV, dtype=torch.int32)).contiguous(), k, v)
+    Q = (k[:, :1, None, :].float() * (16 * D ** 0.5 / k[0, 0].float().square().sum())).to(K.dtype).expand(1, 1, G, D).contiguous()
+    out, lse = torch.empty_like(Q), torch.empty(1, 1, G, device=DEV)
+    c.dynakv_packed_attend(None, Q, None, None, None, out, lse, tree_scratch(1, 1, G, DEV))
+    logit = (Q[0, 0].double() @ k[0].double().T) / D ** 0.5
+    like, weight = float(cap - 50), logit.exp()
+    den = weight.sum(-1) + like
+    one = torch.zeros(D, dtype=torch.float64, device=DEV)
+    one[7] = 1.0
+    want, spread = (weight @ v[0].double() + like * one) / den[:, None], (weight @ v[0].double().abs() + like * one) / den[:, None]
+    assert 0.05 < float(like / den[0]) < 0.95                    # (both kinds count)
+    # The bound: one unit of few rows is shared by 256 workgroups or more, the entries of each by at least four wavefronts, 2^15 entries each; every addition of
+    # such a sum is off by at most u of the sum so far: 2^15 u = 2^-9, for the denominator and for the weighted values.  The weights: the logits'
+    # error and the exponential's, as in _check_tree, and h in 16 bits; float16's small weights are off by half a step of 2^-31 of the largest,
+    # e^-16 of it or more here: 2^-32 e^16 = 0.0021 of each.  An output of float16 below 2^-14 is rounded to steps of 2^-24: off by 2^-25.
+    delta = 132 * U32 * float((Q[0, 0].double().abs() @ k[0].double().abs().T).max()) / D ** 0.5
+    sums = 2.0 ** -9 + 2 * delta + 2.0 ** -21
+    weights = HALF[dt] if dt != "f32" else 0.0
+    if dt == "f16":
+        weights = weights + 2.0 ** -32 * float(logit.max().exp())
+    bound = spread * (2 * sums + weights) * 1.01 + HALF[dt] * want.abs() + (2.0 ** -25 if dt == "f16" else 0.0)
+    assert bool(((out[0, 0].double() - want).abs() <= bound).all())
+    assert bool(((lse[0, 0].double() - den.log()).abs() <= 1.01 * sums + 64 * U32).all())
