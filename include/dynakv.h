@@ -369,7 +369,8 @@ size_t dynakv_tree_scratch_bytes(int32_t n_units, int32_t n_nodes, int32_t group
  *                   A NaN among the logits that a row sees (of a query, of a key) makes its out and lse NaN
  *   scratch         device, 16-byte aligned, at least dynakv_tree_scratch_bytes(U, n_nodes, G) (else DYNAKV_ECAPACITY);
  *                   contents need no initialisation
- * Products and sums are float32; with 16-bit storage a probability is rounded to that type before it weights a value. */
+ * Products and sums are float32; with 16-bit storage a probability is rounded to that type before it weights a value, and the
+ * rounded ones add up to one (lse: those before rounding). */
 dynakv_status_t dynakv_attend_tree(dynakv_index_t* index, const void* Q, int32_t n_nodes, const void* K_tree,
                                    const void* V_tree, const uint64_t* tree, void* out, float* lse, void* scratch,
                                    size_t scratch_bytes, void* stream);

@@ -67,7 +67,7 @@ struct TreeArgs {
   int* where;                                       // [U][2] first piece and pieces of a unit
   float* part;                                      // [pieces][T * G][kPartRow]
 };
-constexpr int kPartRow = kHeadDim + 4;              // accumulators, maximum, denominator, padding to 16 bytes
+constexpr int kPartRow = kHeadDim + 4;              // accumulators, maximum, both sums of weights, padding to 16 bytes
 size_t tree_scratch_bytes(int U, int T, int G);
 hipError_t launch_tree(const TreeArgs& a, hipStream_t st);
 

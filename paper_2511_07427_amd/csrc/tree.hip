@@ -82,6 +82,11 @@ struct Mma {
     if constexpr (DT == DYNAKV_BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2v){x, y}, b2));
     else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2v){x, y}, h2));
   }
+  // c + the sum of two rounded values.
+  static __device__ __forceinline__ float add2(uint32_t w, float c) {
+    if constexpr (DT == DYNAKV_BF16) return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, w), (b2){(__bf16)1.f, (__bf16)1.f}, c, false);
+    else return __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, w), (h2){(_Float16)1.f, (_Float16)1.f}, c, false);
+  }
   // V^T of the 16 entries of chunk c: a group of 16 lanes reads 4 entries (rows) of 16 columns and gets the 4 entries of one column
   // per lane
   struct VFrag { uint4 d[4]; };
@@ -170,6 +175,7 @@ struct Mma<DYNAKV_F32> {
 // Running state of a wavefront's 32 rows: lane l has row l % 32, register i of o[d] column 32 d + entry_of(i, l / 32).
 struct Rows {
   float m, l;                                        // what the weights are relative to (log2), and their sum over the lane's half of the entries
+  float w[2];                                        // the sum of the weights as they go into the products, in two parts (float32: l and 0)
   f16v o[4];
 };
 // Whether a part of a row's entries (a wavefront's, a piece's) has none that the row sees: its sum is 0 then.  The maximum alone does not say so: it
@@ -225,6 +231,8 @@ __device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, 
     const float mn = fmaxf(st.m, mx - kShift<DT>), alpha = mn == st.m ? 1.f : __builtin_amdgcn_exp2f(st.m - mn);
     st.m = mn;
     st.l *= alpha;
+    st.w[0] *= alpha;
+    st.w[1] *= alpha;
 #pragma unroll
     for (int d = 0; d < 4; ++d) st.o[d] *= alpha;
   }
@@ -238,18 +246,23 @@ __device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, 
         p[i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], sc, base));
         sum[i & 3] += p[i];
       }
-      st.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      st.w[0] = st.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       M::pv(st.o, v + n * kSub * M::kRowV, p, lane);
     }
   } else {
     // 16 entries at a time: while the matrix cores take one chunk, the next one's weights are computed and its V is on its way.
-    // A weight goes in rounded to V's type: an error of half a step relative to each term, as much as rounding the output costs.
+    // A weight goes in rounded to V's type: an error of half a step relative to each term, as much as rounding the output costs.  What the sum of products is
+    // divided by is the sum of the rounded weights, so that it is a mean: equal values come out as they are, none beyond the largest (64 of
+    // float16's largest value came out as infinity with the sum before rounding).  The log-sum-exp has the other sum.
     auto weights = [&](int c) {
       float p[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[c >> 1][8 * (c & 1) + i], sc, base));
       st.l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-      return uint4{M::round2(p[0], p[1]), M::round2(p[2], p[3]), M::round2(p[4], p[5]), M::round2(p[6], p[7])};
+      const uint4 r = {M::round2(p[0], p[1]), M::round2(p[2], p[3]), M::round2(p[4], p[5]), M::round2(p[6], p[7])};
+      st.w[0] = M::add2(r.y, M::add2(r.x, st.w[0]));
+      st.w[1] = M::add2(r.w, M::add2(r.z, st.w[1]));
+      return r;
     };
     uint4 w = weights(0);
 #pragma unroll
@@ -563,7 +576,7 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
   }
 
   Rows st;
-  st.m = -__builtin_inff(); st.l = 0.f;
+  st.m = -__builtin_inff(); st.l = 0.f; st.w[0] = st.w[1] = 0.f;
 #pragma unroll
   for (int d = 0; d < 4; ++d) st.o[d] = f16v{};
   char* tiles = lds + grp * Sh::kPlaces * Sh::kTile;
@@ -667,6 +680,8 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
   // join the groups: every wavefront leaves its rows in LDS
   const auto lsum = __builtin_amdgcn_permlane32_swap(__float_as_uint(st.l), __float_as_uint(st.l), false, false);
   st.l = __uint_as_float(lsum[0]) + __uint_as_float(lsum[1]);
+  const float half = st.w[0] + st.w[1];
+  const auto wsum = __builtin_amdgcn_permlane32_swap(__float_as_uint(half), __float_as_uint(half), false, false);
   lds_barrier();
   float* mo = (float*)lds;
   {
@@ -675,13 +690,13 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
     for (int d = 0; d < 4; ++d)
 #pragma unroll
       for (int i = 0; i < 16; i += 4) *(f4*)(at + 32 * d + entry_of(i, h)) = f4{st.o[d][i], st.o[d][i + 1], st.o[d][i + 2], st.o[d][i + 3]};
-    if (h == 0) { at[kHeadDim] = st.m; at[kHeadDim + 1] = st.l; }
+    if (h == 0) { at[kHeadDim] = st.m; at[kHeadDim + 1] = st.l; at[kHeadDim + 2] = __uint_as_float(wsum[0]) + __uint_as_float(wsum[1]); }
   }
   lds_barrier();
   for (int i = threadIdx.x; i < WR * kSub * (kHeadDim / 4); i += Sh::kThreads) {
     const int r = i >> 5, c = (i & 31) * 4, rr = rb * a.rows + r;      // row r of the workgroup: wavefront r / 32 of every group
     if (r >= a.rows || rr >= R) break;
-    float mw[kGroups], m = -__builtin_inff(), l = 0.f;
+    float mw[kGroups], m = -__builtin_inff(), l = 0.f, sum = 0.f;
 #pragma unroll
     for (int w = 0; w < kGroups; ++w) { mw[w] = mo[(w * WR * kSub + r) * kOut + kHeadDim]; m = fmaxf(m, mw[w]); }
     f4 o = {0, 0, 0, 0};
@@ -691,17 +706,18 @@ __global__ __launch_bounds__((Shape<DT, SRC, WR>::kThreads)) void tree_kernel(Tr
       if (saw_nothing(mw[w], x[kHeadDim + 1])) continue;
       const float f = mw[w] == m ? 1.f : __builtin_amdgcn_exp2f(mw[w] - m);
       l += f * x[kHeadDim + 1];
+      sum += f * x[kHeadDim + 2];
       o += f * *(const f4*)(x + c);
     }
     const size_t to = (size_t)u * R + rr;
     if (ns == 1) {
       const bool none = saw_nothing(m, l);
-      M::store4(a.out, to * kHeadDim + c, none ? f4{0, 0, 0, 0} : o / l);
+      M::store4(a.out, to * kHeadDim + c, none ? f4{0, 0, 0, 0} : o / sum);
       if (a.lse && c == 0) a.lse[to] = none ? m : (m + __builtin_amdgcn_logf(l)) * kLn2;
     } else {
       float* p = a.part + ((size_t)piece * R + rr) * kPartRow;
       *(f4*)(p + c) = o;
-      if (c == 0) { p[kHeadDim] = m; p[kHeadDim + 1] = l; }
+      if (c == 0) { p[kHeadDim] = m; p[kHeadDim + 1] = l; p[kHeadDim + 2] = sum; }
     }
   }
 }
@@ -718,12 +734,13 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   const int first = a.where[2 * u], ns = a.where[2 * u + 1];
   if (ns == 1) return;                               // (P = 8: the whole workgroup)
   const float* p = a.part + ((size_t)first * R + r) * kPartRow;
-  float ms[8], ls[8], m = -__builtin_inff(), l = 0.f;
+  float ms[8], ls[8], ws[8], m = -__builtin_inff(), l = 0.f, w = 0.f;
   f4 os[8], o = {0, 0, 0, 0};
-  auto add = [&](float mk, float lk, const f4& ok) {
+  auto add = [&](float mk, float lk, float wk, const f4& ok) {
     if (saw_nothing(mk, lk)) return;
     const float f = mk == m ? 1.f : __builtin_amdgcn_exp2f(mk - m);
     l += f * lk;
+    w += f * wk;
     o += f * ok;
   };
   for (int s0 = grp % P; s0 < ns; s0 += 8 * P) {
@@ -733,6 +750,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
       const float* x = p + (size_t)min(s, ns - 1) * R * kPartRow;
       ms[k] = s < ns ? x[kHeadDim] : -__builtin_inff();
       ls[k] = s < ns ? x[kHeadDim + 1] : 0.f;
+      ws[k] = x[kHeadDim + 2];
       os[k] = *(const f4*)(x + c);
     }
     float top = m;
@@ -741,24 +759,25 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
     const float f = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
     m = top;
     l *= f;
+    w *= f;
     o *= f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) add(ms[k], ls[k], os[k]);
+    for (int k = 0; k < 8; ++k) add(ms[k], ls[k], ws[k], os[k]);
   }
   if constexpr (P == 8) {
     *(f4*)&sm[grp][c] = o;
-    if (c == 0) { sm[grp][kHeadDim] = m; sm[grp][kHeadDim + 1] = l; }
+    if (c == 0) { sm[grp][kHeadDim] = m; sm[grp][kHeadDim + 1] = l; sm[grp][kHeadDim + 2] = w; }
     __syncthreads();
     if (grp > 0) return;
-    m = -__builtin_inff(); l = 0.f;
+    m = -__builtin_inff(); l = 0.f; w = 0.f;
     o = f4{0, 0, 0, 0};
 #pragma unroll
     for (int k = 0; k < 8; ++k) m = fmaxf(m, sm[k][kHeadDim]);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) add(sm[k][kHeadDim], sm[k][kHeadDim + 1], *(const f4*)&sm[k][c]);
+    for (int k = 0; k < 8; ++k) add(sm[k][kHeadDim], sm[k][kHeadDim + 1], sm[k][kHeadDim + 2], *(const f4*)&sm[k][c]);
   }
   const bool none = saw_nothing(m, l);
-  Mma<DT>::store4(a.out, i * kHeadDim + c, none ? f4{0, 0, 0, 0} : o / l);
+  Mma<DT>::store4(a.out, i * kHeadDim + c, none ? f4{0, 0, 0, 0} : o / w);
   if (a.lse && c == 0) a.lse[i] = none ? m : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 

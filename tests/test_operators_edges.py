@@ -1,4 +1,4 @@
-"""Attention of drafted tokens where something that a row sees is NaN, in graphs that hold only a part of it, and in its plainest calls: a token that
+"""Attention of drafted tokens: NaN that a row sees, graphs that hold only a part of it, weights that add up to one, and its plainest calls: a token that
 sees itself, a chain without bits, a denominator of 3e7 like terms.  Bounds are those of test_operators.py unless derived here."""
 import os
 import sys
@@ -229,3 +229,39 @@ def test_every_entry_beyond_32_bits_counts(dt):
     bound = spread * (2 * sums + weights) * 1.01 + HALF[dt] * want.abs() + (2.0 ** -25 if dt == "f16" else 0.0)
     assert bool(((out[0, 0].double() - want).abs() <= bound).all())
     assert bool(((lse[0, 0].double() - den.log()).abs() <= 1.01 * sums + 64 * U32).all())
+
+
+@gpu
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("U,T,G,cap", [(300, 1, 16, 32), (20, 5, 16, 30), (2, 5, 3, 700), (1, 9, 4, 3000), (3, 40, 8, 900)])
+def test_equal_values_come_out_as_they_are(dt, U, T, G, cap):
+    """A mean of equal values, with equal weights but for one, so that all are rounded alike: whatever a weight is rounded to, the weights add up to one.  What
+    is left are float32 sums, (3000 / 4 + 64) u = 5e-5 at most, which the output's rounding, half a step of 2^-12 or more of a value of 16 bits, takes back."""
+    gen = torch.Generator(DEV).manual_seed(U + T + cap)
+    value = torch.arange(D, device=DEV).remainder(32) + 96.0     # codes of 8 bits with scale 1
+
+    def spoil(K, V):
+        V[:], K[:, 2:] = value, K[:, 1:2].clone()
+    c, K, V = _filled(dt, 8, U, cap, gen, spoil)
+    Q, K1, V1, out, lse = _drafts(dt, U, T, G, gen)
+    V1[:], K1[:] = value, K[:, 1:2]
+    c.dynakv_packed_attend(None, Q, K1, V1, None, out, lse, tree_scratch(U, T, G, DEV))
+    assert torch.equal(out.float(), value.expand_as(out))
+
+
+@gpu
+def test_the_largest_values_stay_finite():
+    """32 drafted tokens with the largest value of float16, one with weight 1, the others with a weight whose rounding to 11 bits goes up by almost half a step,
+    1/2 (1 + 0.51 2^-10).  Weights whose sum is taken before they are rounded would give 1.00045 times that value: infinity."""
+    T = 32
+    Q, K1 = (torch.zeros(1, T, *s, D, dtype=torch.float16, device=DEV) for s in ((1,), ()))
+    logit = torch.log(torch.tensor(0.5 * (1 + 0.51 * 2.0 ** -10), dtype=torch.float64))
+    Q[..., 0], Q[..., 1] = 1.0, 2.0 ** -11
+    K1[:, 1:, 0] = logit.half().item()
+    K1[:, 1:, 1] = (logit - logit.half().double()).item() * 2.0 ** 11
+    V1 = torch.full_like(K1, torch.finfo(torch.float16).max)
+    out, lse = torch.empty_like(Q), torch.empty(1, T, 1, device=DEV)
+    c = PackedCache.zeros(1, 1, "f16", 8, DEV)
+    c.dynakv_packed_attend(torch.zeros(1, dtype=torch.int32, device=DEV), Q, K1, V1, torch.full((1, T), -1, dtype=torch.int64, device=DEV), out, lse,
+                           tree_scratch(1, T, 1, DEV), softmax_scale=1.0)
+    assert torch.equal(out, V1[0, 0].expand_as(out))
