@@ -80,7 +80,7 @@ __device__ __forceinline__ void exchange(T& x, T& y, bool upper) {
 
 // Workgroup (16 / HP tokens, chunk of HP a.per heads); HP rows of 16 lanes belong to a token, each takes `per` heads, kBatch of them on their way
 // at once.  All rows go the same way through the code, values too (their result is dropped): with branches and 64-bit address arithmetic per
-// kind of row the kernel had as much to issue as to move (191 us for 16384 tokens of 80 bfloat16 rows; now 138 to 151, 4.5 to 4.9 TB/s).
+// kind of row the kernel had as much to issue as to move (191 us for 16384 tokens of 80 bfloat16 rows; now 134, 5.0 TB/s).
 template <int DT, int ORDER, int HP, bool STREAM>
 __global__ __launch_bounds__(256) void norm_rope_kernel(HeadsArgs a) {
   using F = Four<DT>;
@@ -221,8 +221,9 @@ template <int DT, int ORDER>
 hipError_t launch(HeadsArgs& a, hipStream_t st) {
   const int heads = a.c.n_kv_heads * (a.c.group_size + 2);
   const long long tokens = (long long)a.c.n_seqs * a.c.n_tokens;
-  // Few tokens: one head to a row of lanes, so that the chip has work (one token of 48 rows 3.9 us, as many would be 4.2).  Many: the angles of a token are what its rows of lanes each work out, for
-  // kBatch heads or more, so few rows share a token (5664 tokens of 9 heads: 18.6 us with 16 rows each, 15.4 with 8, 12.3 with 4).
+  // Few tokens: one head to a row of lanes, so that the chip has work (one token of 48 rows 3.9 us, as many would be 4.2).  Many: the angles of a
+  // token are what its rows of lanes each work out, for kBatch heads or more, so few rows share a token (5664 tokens of 9 heads: 18.6 us with 16 rows
+  // each, 15.4 with 8, 12.3 with 4).
   const bool many = tokens * ((heads + 15) / 16) > 2048;
   const int hp = many ? (heads > 32 ? 16 : heads > 16 ? 8 : 4) : heads > 8 ? 16 : heads > 4 ? 8 : 4;
   a.per = many ? 8 : 1;

@@ -51,7 +51,8 @@ struct TreeArgs {
   void* out;
   float* lse;
   void* scratch;
-  int most;                                         // no unit has more entries than this, as far as the host knows
+  int most;                                         // what the cut is planned for: a unit's tokens at most, as far as the host knows (the capacity, the
+                                                    // budget; a list of clusters of one token has four slots for each, of which one is used)
   // the entries: the gather list of an index ...
   const char* pages;                                // null: a packed cache
   size_t unit_pages;                                // bytes of a unit's page pool

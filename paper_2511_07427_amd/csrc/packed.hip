@@ -5,8 +5,9 @@
 // rounding, so the codes are those of exact arithmetic, and reading back rounds nothing.  Both directions are bound by
 // memory: a row is 128 elements and 132 or 68 bytes.  16 lanes hold a row, 8 values each, so that a lane's loads and stores of 16-bit values
 // are 16 bytes wide and the rows of a wavefront lie one after the other; a block is one quad of lanes, and its maximum crosses them in two steps.
-// 256 units of 4096 float16 tokens to 4 bits: writing 136 us (5.0 TB/s), reading 141 (4.8); reading 112 of 8192 bfloat16
-// tokens from 8 bits 125 us (5.7).
+// 256 units of 4096 float16 tokens to 4 bits: writing 126 us (5.4 TB/s), reading 141 (4.9); reading 112 of 8192 bfloat16
+// tokens from 8 bits 125 us (5.7).  Rows at scattered positions cost more than their bytes: a row's codes and scales lie in four places, of each of which
+// memory gives 128 bytes (32768 rows of 136 bytes: 15.8 MiB read for 4.3).
 #include "operators.hpp"
 
 namespace dynakv {

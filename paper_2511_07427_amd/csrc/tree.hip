@@ -197,14 +197,15 @@ __device__ __forceinline__ f16v begin_scores(const float* bias, int lane) {
 // N tiles of 32 entries.  Of a tile of the cache every row sees the same slots, those with a bias of 0; of drafted tokens (their bias is 0) those
 // whose bit is set in `seen`.  Slots that hold nothing have zeros in K and V.
 // The accumulators are rescaled only when a maximum has grown by more than 2^kLazy since they last were: until then weights grow up to that,
-// and 64 products per tile and row are saved in all but a few tiles (3 % of the time of 128 packed units of 128 rows).  Weights are relative to 2^-kShift times the maximum: those of float16, whose
-// smallest step is 2^-24, so reach down to 2^-31 of the largest (many small ones beside a large one count), and stay below 2^15.
+// and 64 products per tile and row are saved in all but a few tiles (half a percent of the time of 128 packed units of 128 rows, one percent of that of
+// 112 units of 427 rows).  Weights are relative to 2^-kShift times the maximum: those of float16, whose smallest step is 2^-24, so reach down to 2^-31 of the largest
+// (many small ones beside a large one count), and stay below 2^15.
 constexpr float kLazy = 8.f;
 template <int DT>
 constexpr float kShift = DT == DYNAKV_F16 ? 7.f : 0.f;
 template <int DT, int N>
-__device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, const float* bias, const typename Mma<DT>::Q& q, bool drafts, unsigned long long seen, float sc,
-                                        int lane) {
+__device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, const float* bias, const typename Mma<DT>::Q& q, bool drafts,
+                                        unsigned long long seen, float sc, int lane) {
   using M = Mma<DT>;
   f16v s[N];
 #pragma unroll
@@ -396,7 +397,8 @@ __device__ __forceinline__ void spread(char* to, uint4 w4, float scale) {
         for (int k = 0; k < 4; ++k) o[k] = __float_as_uint(x[k]);
       } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] = __builtin_amdgcn_perm(__float_as_uint(x[2 * k + 1]), __float_as_uint(x[2 * k]), 0x07060302u);   // exact: the lower halves are zero
+        for (int k = 0; k < 4; ++k)                  // exact: the lower halves are zero
+          o[k] = __builtin_amdgcn_perm(__float_as_uint(x[2 * k + 1]), __float_as_uint(x[2 * k]), 0x07060302u);
       }
       *(uint4*)(to + 16 * c) = uint4{o[0], o[1], o[2], o[3]};
     }
@@ -519,13 +521,15 @@ struct Drafts {
 // A workgroup of W wavefronts, one per compute unit: WR of them take 32 rows each and share tiles of kSlots entries; W / WR such groups take
 // the tiles in turn.  Shared tiles have two places, of which one is filled while the other is read, with one barrier per tile.  A wavefront
 // that has its tiles alone (up to 32 rows: bound by memory) keeps 32 rows of K and V on their way in registers: 128 KB per compute unit.
-// Measured: 8 units of 131072 entries in 8 bits, one node of 8 heads: 58 us, 4.8 TB/s of codes and scales.  112 units of 2048 gathered entries and
-// 427 rows: 79 to 91 us; the matrix units are busy 36 % of that, vector instructions 44 %, LDS 39 %: no unit alone bounds it.  The two wavefronts of
-// a SIMD half a round apart, one reading keys while the other takes exponentials (two barriers a round), took 87.
+// Measured after 30 ms of work (a card that was idle takes up to a quarter longer until then): 8 units of 131072 entries in 8 bits, one node of
+// 8 heads: 56 us, 4.9 TB/s of codes and scales.  112 units of 2048 gathered entries and 427 rows: 83 us; the matrix units are busy 34 % of that, vector
+// instructions 44 %, LDS 36 %: no unit alone bounds it.  The two wavefronts of a SIMD half a round apart, one reading keys while the other takes
+// exponentials (two barriers a round), took 87 where this order took 79, both with one sum of the weights.
 template <int DT, int SRC, int WR>
 struct Shape {
   static constexpr int W = DT == DYNAKV_F32 ? 4 : 8, kThreads = 64 * W;
-  static constexpr int kGroups = W / WR, kSlots = WR >= 4 ? 2 * kSub : kSub, kMine = kSlots / WR, kPlaces = WR == 1 ? 1 : 2;   // kMine: rows of a tile that a wavefront loads
+  static constexpr int kGroups = W / WR, kSlots = WR >= 4 ? 2 * kSub : kSub, kPlaces = WR == 1 ? 1 : 2;
+  static constexpr int kMine = kSlots / WR;                                                         // rows of a tile that a wavefront loads
   static constexpr int kTileK = kSlots * Mma<DT>::kRowK, kTileV = kSlots * Mma<DT>::kRowV, kTile = kTileK + kTileV + kSlots * 4;   // bytes: K, V, bias
   static constexpr int kOut = kHeadDim + 4;                                                         // floats of a row in the merge
   static constexpr int kMerge = W * kSub * kOut * 4, kTiles = kGroups * kPlaces * kTile, kLds = kTiles > kMerge ? kTiles : kMerge;
@@ -782,10 +786,10 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
 }
 
 // Most wavefronts of a workgroup that take rows of their own, up to eight times 32 of the R rows of a unit: what they read of LDS they share with none,
-// what they load and unpack with all.  R = 427, 2048 entries of 112 units: 171 us with one, 147 with two, 108 with four, 92 with eight; R = 128 of
-// 128 packed units: 136, 108, 69 with four.  For 32 rows a second wavefront would be idle: 8 long packed units 62 us, with two 78.  Several blocks of
-// rows are made alike (R = 427: seven wavefronts of eight twice, 88 us, instead of eight and six, 92).  A float32 wavefront's queries and sums
-// leave room for one on a SIMD; its matrix instructions are what bounds it, whoever loads the tiles.
+// what they load and unpack with all.  R = 427, 2048 entries of 112 units: 169 us with one, 147 with two, 103 with four, 83 with eight; R = 128 of
+// 128 packed units: 130, 94, 71 with four.  For 32 rows a second wavefront would be idle: 8 long packed units 60 us, with two 72.  Several blocks of
+// rows are made alike (R = 427: seven wavefronts of eight twice, 82.7 us, eight and six 82.9).  A float32 wavefront's queries and sums leave room
+// for one on a SIMD; its matrix instructions are what bounds it, whoever loads the tiles.
 int row_waves(int dtype, int R) { return dtype == DYNAKV_F32 || R <= kSub ? 1 : R <= 2 * kSub ? 2 : R <= 4 * kSub ? 4 : 8; }
 
 // How the work is cut: `waves` of a workgroup take rows of their own, `pieces` are the workgroups that a call gets for each block of rows, `least` the
@@ -793,9 +797,13 @@ int row_waves(int dtype, int R) { return dtype == DYNAKV_F32 || R <= kSub ? 1 : 
 // and 0.7 for each of its waves to begin and end, and per entry the larger of its bytes (at its share of 5 TB/s, at most 64 per ns, 36 where waves
 // share tiles) and the work of its rows, 4 for each 32 (34 for float32's matrix instructions), and 4 or (not float16) 10 to unpack; the kernel that
 // joins takes 6 us.  Units of one length would be cut into s pieces each; a multiple of 256 workgroups that has room for those is what units of any
-// lengths share, which then weigh three quarters of the longest.  (8 units of 131072 packed entries: 62 us, whole 1247; 128 units of up to 8191: 69,
-// whole 146.)  Fewer waves than there could be make more blocks of rows, for chips that would be idle otherwise: 5 units of 352 rows and 272
-// entries 11 us (as many waves as could be: 19), 81 of 255 and 417 22 (32), 140 of 336 and 761 56 (77).
+// lengths share, which then weigh three quarters of the longest.  (8 units of 131072 packed entries: 60 us, whole 1270; 128 units of up to 8191: 71,
+// whole 108.)  Fewer waves than there could be make more blocks of rows, for chips that would be idle otherwise: 5 units of 352 rows and 272
+// entries 11 us (as many waves as could be: 19), 81 of 255 and 417 22 (34), 140 of 336 and 761 54 (73).
+// The model's own numbers, over 60 calls of the sizes of a batch: another cut for 3 % (or for any gain, or for 10 %), half or all of the longest instead of
+// three quarters, at most two or eight rounds: 1 % on the mean either way, single calls 8 % shorter to 6 % longer.  Fewer waves for 10 %: for any
+// gain 1 % either way, for 25 % single calls take up to 1.58 times as long.
+// More than kPlanUnits units fill the chip whole: 700 of up to 4096 packed entries 119 us, shared 133; 1000: 157, 193; alike 158, 174 and 224, 237.
 struct Plan { int waves, pieces, least; };
 constexpr int kMostRounds = 4;                       // bounds the scratch
 // Fewer waves than there could be make at most this many workgroups of 512: a launch has fewer than 2^32 work-items.  (As many as could be make a
