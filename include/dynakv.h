@@ -320,8 +320,9 @@ dynakv_status_t dynakv_norm_rope(const dynakv_heads_t* heads, const void* q, con
 /* A packed cache: one row of K and one of V per unit and position, every 32 neighbouring values as integers c of `bits` bits
  * (|c| <= 127 or 7) and one scale, a power of two: value = c * 2^(s - 127), s the scale's byte.  The writer takes the
  * smallest scale that cuts no value off (2^e, -126 <= e; of float16: -24 <= e; so large that 127 or 7 times it still is a
- * finite value: values beyond are held as that one) and rounds to the nearest code, ties to even.  Every value so held is exactly a value
- * of `dtype`: what is read back is what the attention sees (a cache that is filled otherwise keeps to these scales).  A block with a value that is not finite is held as s = 255 and is
+ * finite value: values beyond are held as that one) and rounds to the nearest code, ties to even.  Every value so held is
+ * exactly a value of `dtype`: what is read back is what the attention sees (a cache that is filled otherwise keeps to these
+ * scales).  A block with a value that is not finite is held as s = 255 and is
  * NaN throughout.  4-bit codes lie two to a byte, the even one in the low half, in two's complement, like those of 8 bits. */
 typedef struct {
   int32_t n_units;     /* U >= 1                                                       */
