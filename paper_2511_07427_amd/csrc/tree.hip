@@ -198,8 +198,8 @@ __device__ __forceinline__ f16v begin_scores(const float* bias, int lane) {
 // whose bit is set in `seen`.  Slots that hold nothing have zeros in K and V.
 // The accumulators are rescaled only when a maximum has grown by more than 2^kLazy since they last were: until then weights grow up to that,
 // and 64 products per tile and row are saved in all but a few tiles (half a percent of the time of 128 packed units of 128 rows, one percent of that of
-// 112 units of 427 rows).  Weights are relative to 2^-kShift times the maximum: those of float16, whose smallest step is 2^-24, so reach down to 2^-31 of the largest
-// (many small ones beside a large one count), and stay below 2^15.
+// 112 units of 427 rows).  Weights are relative to 2^-kShift times the maximum: those of float16, whose smallest step is 2^-24, so reach down to
+// 2^-31 of the largest (many small ones beside a large one count), and stay below 2^15.
 constexpr float kLazy = 8.f;
 template <int DT>
 constexpr float kShift = DT == DYNAKV_F16 ? 7.f : 0.f;
@@ -253,8 +253,9 @@ __device__ __forceinline__ void consume(Rows& st, const char* k, const char* v, 
   } else {
     // 16 entries at a time: while the matrix cores take one chunk, the next one's weights are computed and its V is on its way.
     // A weight goes in rounded to V's type: an error of half a step relative to each term, as much as rounding the output costs.  What the sum of products is
-    // divided by is the sum of the rounded weights, so that it is a mean: equal values come out as they are, none beyond the largest (64 of
-    // float16's largest value came out as infinity with the sum before rounding).  The log-sum-exp has the other sum.
+    // divided by is the sum of the rounded weights, so that it is a mean: equal values come out as they are, none beyond the largest (32 of
+    // float16's largest value came out as infinity with the sum before rounding).  The log-sum-exp has the other sum.  Both sums: 61 nodes on 112
+    // bfloat16 units 84 us, one 80; the error against 64 bits 1.75e-3 instead of 1.88e-3 of the norm.
     auto weights = [&](int c) {
       float p[8];
 #pragma unroll
